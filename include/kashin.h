@@ -52,6 +52,10 @@ enum {
  * and bfloat16 (the upper half of a binary32; widened exactly). */
 enum { KASHIN_F32 = 0, KASHIN_F16 = 1, KASHIN_BF16 = 2 };
 
+/* 8-bit floats (OCP e4m3: largest 448, no infinities) that stand for value x scale, one fp32 scale for
+ * each row or group of entries: written by kashin_rmsnorm, read by the kashin_matmul entry points. */
+enum { KASHIN_E4M3 = 3 };
+
 /* 1 if vectors of length n have a compiled kernel, else 0.  Host only, no device needed.
  * The supported lengths are exactly
  *     64, 96, 172, 256, 512, 768, 1024, 2048, 3072, 4096, 5120, 6144, 8192, 10000, 11008,
@@ -292,6 +296,78 @@ int kashin_optq_quantize_noalloc(kashin_plan_t plan, float* w_t, int64_t d_in, i
                                  const double* v, int64_t ldu, int64_t quantize_rows, int32_t chunk, int32_t exact,
                                  int32_t lloyd_iters, uint8_t* codes_u, uint8_t* codes_v, float* centers, float* q_t,
                                  void* stream);
+
+/* The operators of a quantised model's layers: the norm in front of a layer and the products with the
+ * codes themselves, so that W_hat is never put together (App. C: X W_hat^T = [X | X P] [U | V]^T).
+ *
+ * kashin_rmsnorm: for each of t rows of n entries, s = x + r (fp32), h = s rounded to the rows' type (the
+ * residual stream's next value) and
+ *     y = s * rsqrt(mean(s^2) + eps) * weight.
+ * In 8 bits (y_dtype KASHIN_E4M3), for each group of `group` consecutive entries (the last one of a row may
+ * be shorter; group 0: the row), scale = max|y| / 448 and y8 = y / scale rounded to the nearest e4m3.
+ *   x       t rows of n, 1 <= n <= 16384 (else KASHIN_E_UNSUPPORTED_N), dtype KASHIN_F32, _F16 or _BF16,
+ *           ldx >= n (device)
+ *   r       the residual, of x's type, ldr >= n (device, nullable: s = x)
+ *   weight  n entries of x's type (device, nullable: ones); eps >= 0
+ *   h       t rows of x's type, ldh >= n (device, nullable); h may be x or r (the same rows), any other
+ *           overlap with them is KASHIN_E_INVALID
+ *   y       t rows of y_dtype KASHIN_F32, _F16, _BF16 or _E4M3, ldy >= n (device); overlaps none of the others
+ *   scales  t x ceil(n / group) fp32, or t for group 0 (device): KASHIN_E4M3 only, else null and group 0
+ *   group   0, 32, 64, 128 or 256
+ * Sums are fp32: a row whose sum of squares passes 3.4e38 gives zeros.  A row holding NaN or Inf gives NaN
+ * where y is; in 8 bits, a group holding NaN has scale NaN and zeros.  A group of zeros has scale 0.
+ * Plan-free: runs on the current device. */
+int kashin_rmsnorm(int64_t t, int32_t n, const void* x, int32_t dtype, int64_t ldx, const void* r, int64_t ldr,
+                   const void* weight, float eps, void* h, int64_t ldh, void* y, int32_t y_dtype, int64_t ldy,
+                   float* scales, int32_t group, void* stream);
+
+/* A quantised matrix W_hat (m x k, k = groups * n, n the plan's length) as the quantiser leaves it: row i of
+ * group g is row i * groups + g of the codes and centres (kashin_quantize of W seen as m * groups rows of n),
+ * w = u_q + P v_q, or R^T (u_q + P v_q) where rot_seed is given.  experts > 1: that many such matrices one
+ * behind the other (expert e's rows start at e * m * groups), all with this plan and rotation. */
+typedef struct {
+  kashin_plan_t plan;
+  const uint64_t* rot_seed; /* host, nullable: the rotation's seed (lengths of kashin_rotate) */
+  const uint8_t* codes_u;   /* experts * m * groups rows of ceil(n/4) bytes (device) */
+  const uint8_t* codes_v;   /* the same (device) */
+  const float* centers;     /* experts * m * groups x 2 x 4 (device) */
+  int64_t m;                /* 1 <= m <= 2^24 */
+  int32_t groups;           /* groups >= 1, k <= 2^20 */
+  int32_t experts;          /* 1 <= experts <= 1024 (1 but for kashin_matmul_experts) */
+} kashin_weights;
+
+/* Device workspace bytes that the products need for t rows (0 <= t <= 2^16); -1 for bad sizes.  `transposed`
+ * 0: kashin_matmul, 1: kashin_matmul_t. */
+int64_t kashin_matmul_workspace_bytes(int32_t n, int64_t m, int32_t groups, int64_t t, int32_t experts,
+                                      int32_t transposed);
+
+/* y = x W_hat^T (t x k by m x k): x's rows against the matrix's rows, from one token to a prompt.
+ *   x         t rows of k, dtype KASHIN_F32, _F16, _BF16 or _E4M3, ldx >= k (device)
+ *   x_scales  KASHIN_E4M3: t x ceil(k / x_group) fp32 scales (x_group a multiple of 32), or t (x_group 0: one
+ *             for each row); else null and x_group 0 (device)
+ *   y         t rows of m, y_dtype KASHIN_F32, _F16 or _BF16, ldy >= m (device); overlaps neither x nor work
+ *   work      at least kashin_matmul_workspace_bytes(n, m, groups, t, experts, 0) bytes, 16-byte aligned
+ *             (device; its contents on entry do not matter; calls that overlap in time need one each)
+ * P x and sums are fp32; the products are exact to about 2^-21 of a row's largest terms, and to 2^-11 of
+ * them at most where y is bf16 and t > 16.  A row of x holding NaN or Inf gives a row of NaN, a row of W_hat with a
+ * centre that is not finite gives a column of NaN. */
+int kashin_matmul(const kashin_weights* w, const void* x, int32_t x_dtype, int64_t t, int64_t ldx, const float* x_scales,
+                  int32_t x_group, void* y, int32_t y_dtype, int64_t ldy, void* work, int64_t work_bytes, void* stream);
+
+/* y = x W_hat (t x m by m x k), y t rows of k: the product with codes that are held transposed (the rows that
+ * kashin_optq_quantize leaves are W's columns), and the gradient of kashin_matmul with respect to x (x there:
+ * the gradient of its y).  Arguments as kashin_matmul with x's rows of m and y's of k. */
+int kashin_matmul_t(const kashin_weights* w, const void* x, int32_t x_dtype, int64_t t, int64_t ldx,
+                    const float* x_scales, int32_t x_group, void* y, int32_t y_dtype, int64_t ldy, void* work,
+                    int64_t work_bytes, void* stream);
+
+/* Either product grouped by expert: rows offsets[e] .. offsets[e + 1] - 1 of x and y with expert e's matrix, e <
+ * experts.  offsets: experts + 1 int64 (device), not decreasing, within [0, t] (values outside are taken as the
+ * nearest bound).  Rows of y before offsets[0] and from offsets[experts] on are left as they were; their
+ * rows of x may hold anything.  transposed: 0 as kashin_matmul, 1 as kashin_matmul_t. */
+int kashin_matmul_experts(const kashin_weights* w, const int64_t* offsets, int32_t transposed, const void* x,
+                          int32_t x_dtype, int64_t t, int64_t ldx, const float* x_scales, int32_t x_group, void* y,
+                          int32_t y_dtype, int64_t ldy, void* work, int64_t work_bytes, void* stream);
 
 /* Static text for a status code. */
 const char* kashin_status_string(int status);

@@ -49,8 +49,9 @@ def _hipcc() -> str:
 
 def sources() -> list[str]:
     srcs = [os.path.join(CSRC, "kashin_api.cpp"), os.path.join(CSRC, "kashin_dispatch.hip"),
-            os.path.join(CSRC, "kashin_rotate.hip"), os.path.join(CSRC, "kashin_optq.hip")]
-    srcs += sorted(glob.glob(os.path.join(CSRC, "kashin_n*.hip")))
+            os.path.join(CSRC, "kashin_rotate.hip"), os.path.join(CSRC, "kashin_optq.hip"),
+            os.path.join(CSRC, "kashin_norm.hip"), os.path.join(CSRC, "kashin_matmul.hip")]
+    srcs += sorted(glob.glob(os.path.join(CSRC, "kashin_n[0-9]*.hip")))
     return srcs
 
 

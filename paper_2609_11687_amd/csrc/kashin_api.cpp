@@ -708,6 +708,172 @@ int kashin_optq_quantize_noalloc(kashin_plan_t plan, float* w_t, int64_t d_in, i
                   centers, q_t, static_cast<char*>(work), stream);
 }
 
+namespace {
+
+int64_t elem_size(int32_t dtype) { return dtype == KASHIN_F32 ? 4 : dtype == KASHIN_E4M3 ? 1 : 2; }
+
+// Rows of `width` entries: the addresses from the first entry to behind the last.
+struct Span {
+  uintptr_t lo, hi;
+  Span(const void* p, int64_t rows, int64_t ld, int64_t width, int64_t size)
+      : lo(reinterpret_cast<uintptr_t>(p)), hi(p == nullptr || rows == 0 ? lo : lo + ((rows - 1) * ld + width) * size) {}
+  bool meets(const Span& o) const { return lo < o.hi && o.lo < hi; }
+};
+
+// The plan's device is made current for the call and the caller's restored.
+struct DeviceScope {
+  int before = 0;
+  hipError_t error;
+  bool changed = false;
+  explicit DeviceScope(int device) : error(hipGetDevice(&before)) {
+    if (error == hipSuccess && before != device) {
+      error = hipSetDevice(device);
+      changed = error == hipSuccess;
+    }
+  }
+  ~DeviceScope() {
+    if (changed) (void)hipSetDevice(before);
+  }
+};
+
+bool product_sizes_ok(int32_t n, int64_t m, int32_t groups, int64_t t, int32_t experts) {
+  return kashin_supported_n(n) && m >= 1 && m <= kashin::kProductMaxM && groups >= 1 &&
+         groups <= kashin::kProductMaxK / n && t >= 0 && t <= kashin::kProductMaxRows && experts >= 1 &&
+         experts <= kashin::kProductMaxExperts;
+}
+
+int product(const kashin_weights* w, const int64_t* offsets, bool grouped, bool back, const void* x, int32_t x_dtype,
+            int64_t t, int64_t ldx, const float* x_scales, int32_t x_group, void* y, int32_t y_dtype, int64_t ldy,
+            void* work, int64_t work_bytes, void* stream) {
+  if (w == nullptr) return fail(KASHIN_E_INVALID, "w is null");
+  if (!live(w->plan)) return fail(KASHIN_E_INVALID, "plan is null or destroyed");
+  const kashin_plan_s* p = w->plan;
+  if (!product_sizes_ok(p->n, w->m, w->groups, t, w->experts))
+    return fail(KASHIN_E_INVALID, "m (%lld), groups (%d), experts (%d) or t (%lld) out of range", (long long)w->m,
+                w->groups, w->experts, (long long)t);
+  if (!grouped && w->experts != 1)
+    return fail(KASHIN_E_INVALID, "experts must be 1 here (got %d)", w->experts);
+  if (w->rot_seed != nullptr && !kashin::rotate_supported_n(p->n))
+    return fail(KASHIN_E_UNSUPPORTED_N, "n = %d: the rotation needs n <= 16384 with odd part 1, 3 or 43", p->n);
+  if (!dtype_ok(x_dtype) && x_dtype != KASHIN_E4M3)
+    return fail(KASHIN_E_INVALID, "x_dtype must be F32, F16, BF16 or E4M3");
+  if (!dtype_ok(y_dtype)) return fail(KASHIN_E_INVALID, "y_dtype must be F32, F16 or BF16");
+  const int64_t k = int64_t(w->groups) * p->n, wx = back ? w->m : k, wy = back ? k : w->m;
+  if (ldx < wx || ldy < wy)
+    return fail(KASHIN_E_INVALID, "ldx (%lld) < %lld or ldy (%lld) < %lld", (long long)ldx, (long long)wx,
+                (long long)ldy, (long long)wy);
+  if (x_dtype == KASHIN_E4M3) {
+    if (x_group < 0 || x_group % 32 != 0) return fail(KASHIN_E_INVALID, "x_group must be 0 or a multiple of 32");
+  } else if (x_scales != nullptr || x_group != 0) {
+    return fail(KASHIN_E_INVALID, "x_scales and x_group belong to E4M3 rows");
+  }
+  if (t == 0) return ok();
+  if (!w->codes_u || !w->codes_v || !w->centers || !x || !y || (x_dtype == KASHIN_E4M3 && !x_scales) ||
+      (grouped && !offsets))
+    return fail(KASHIN_E_INVALID, "codes, centers, x, y%s%s must be non-null", grouped ? ", offsets" : "",
+                x_dtype == KASHIN_E4M3 ? ", x_scales" : "");
+  const int64_t need = kashin::product_workspace_bytes(p->n, w->m, w->groups, t, w->experts, back);
+  if (!work || work_bytes < need || reinterpret_cast<uintptr_t>(work) % 16 != 0)
+    return fail(KASHIN_E_INVALID, "work must hold %lld bytes at a 16-byte boundary (got %lld)", (long long)need,
+                (long long)work_bytes);
+  const Span sx(x, t, ldx, wx, elem_size(x_dtype)), sy(y, t, ldy, wy, elem_size(y_dtype)), sw(work, 1, 0, need, 1);
+  if (sy.meets(sx) || sy.meets(sw) || sx.meets(sw)) return fail(KASHIN_E_INVALID, "x, y and work overlap");
+  kashin::ProductArgs a;
+  a.p = base_args(p, kashin::MODE_APPLY_P);
+  a.n = p->n;
+  a.m = w->m;
+  a.groups = w->groups;
+  a.experts = w->experts;
+  a.back = back;
+  a.codes_u = w->codes_u;
+  a.codes_v = w->codes_v;
+  a.centers = w->centers;
+  a.offsets = grouped ? offsets : nullptr;
+  a.rot = w->rot_seed != nullptr;
+  a.rot_seed = a.rot ? *w->rot_seed : 0;
+  a.x = x;
+  a.x_dtype = x_dtype;
+  a.t = t;
+  a.ldx = ldx;
+  a.x_scales = x_scales;
+  a.x_group = x_group;
+  a.y = y;
+  a.y_dtype = y_dtype;
+  a.ldy = ldy;
+  a.work = static_cast<char*>(work);
+  const DeviceScope on(p->device);
+  if (on.error != hipSuccess) return hip_fail(on.error, "the plan's device");
+  const hipError_t e = kashin::launch_product(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "kernel launch");
+  return ok();
+}
+
+}  // namespace
+
+int kashin_rmsnorm(int64_t t, int32_t n, const void* x, int32_t dtype, int64_t ldx, const void* r, int64_t ldr,
+                   const void* weight, float eps, void* h, int64_t ldh, void* y, int32_t y_dtype, int64_t ldy,
+                   float* scales, int32_t group, void* stream) {
+  if (n < 1 || n > kashin::kNormMaxN)
+    return fail(KASHIN_E_UNSUPPORTED_N, "n must be in [1, %d] (got %d)", kashin::kNormMaxN, n);
+  if (t < 0) return fail(KASHIN_E_INVALID, "t must be >= 0 (got %lld)", (long long)t);
+  if (!dtype_ok(dtype)) return fail(KASHIN_E_INVALID, "dtype must be F32, F16 or BF16");
+  if (!dtype_ok(y_dtype) && y_dtype != KASHIN_E4M3)
+    return fail(KASHIN_E_INVALID, "y_dtype must be F32, F16, BF16 or E4M3");
+  if (!(eps >= 0.f) || !(eps <= 1e30f)) return fail(KASHIN_E_INVALID, "eps must be finite and >= 0");
+  if (ldx < n || ldy < n || (r && ldr < n) || (h && ldh < n))
+    return fail(KASHIN_E_INVALID, "a leading dimension is < n (%d)", n);
+  if (y_dtype == KASHIN_E4M3) {
+    if (group != 0 && group != 32 && group != 64 && group != 128 && group != 256)
+      return fail(KASHIN_E_INVALID, "group must be 0, 32, 64, 128 or 256 (got %d)", group);
+  } else if (scales != nullptr || group != 0) {
+    return fail(KASHIN_E_INVALID, "scales and group belong to E4M3 rows");
+  }
+  if (t == 0) return ok();
+  if (!x || !y || (y_dtype == KASHIN_E4M3 && !scales))
+    return fail(KASHIN_E_INVALID, "x, y%s must be non-null", y_dtype == KASHIN_E4M3 ? ", scales" : "");
+  const int64_t esz = elem_size(dtype), per_row = group ? (n + group - 1) / group : 1;
+  const Span sx(x, t, ldx, n, esz), sr(r, t, ldr, n, esz), sh(h, t, ldh, n, esz), sy(y, t, ldy, n, elem_size(y_dtype)),
+      sw(weight, 1, 0, n, esz), ss(scales, 1, 0, t * per_row, 4);
+  const bool h_is_x = h == x && ldh == ldx, h_is_r = h == r && ldh == ldr;
+  if ((sh.meets(sx) && !h_is_x) || (sh.meets(sr) && !h_is_r))
+    return fail(KASHIN_E_INVALID, "h overlaps x or r without being the same rows");
+  if (sy.meets(sx) || sy.meets(sr) || sy.meets(sh) || sy.meets(sw) || sy.meets(ss) || sh.meets(sw) || sh.meets(ss) ||
+      ss.meets(sx) || ss.meets(sr) || ss.meets(sw))
+    return fail(KASHIN_E_INVALID, "an output overlaps another argument");
+  const kashin::NormArgs a = {t, n, x, ldx, r, ldr, weight, eps, h, ldh, y, y_dtype, ldy, scales, group};
+  const hipError_t e = kashin::launch_rmsnorm(a, dtype, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "kernel launch");
+  return ok();
+}
+
+int64_t kashin_matmul_workspace_bytes(int32_t n, int64_t m, int32_t groups, int64_t t, int32_t experts,
+                                      int32_t transposed) {
+  if (!product_sizes_ok(n, m, groups, t, experts) || (transposed != 0 && transposed != 1)) return -1;
+  return kashin::product_workspace_bytes(n, m, groups, t, experts, transposed != 0);
+}
+
+int kashin_matmul(const kashin_weights* w, const void* x, int32_t x_dtype, int64_t t, int64_t ldx, const float* x_scales,
+                  int32_t x_group, void* y, int32_t y_dtype, int64_t ldy, void* work, int64_t work_bytes,
+                  void* stream) {
+  return product(w, nullptr, false, false, x, x_dtype, t, ldx, x_scales, x_group, y, y_dtype, ldy, work, work_bytes,
+                 stream);
+}
+
+int kashin_matmul_t(const kashin_weights* w, const void* x, int32_t x_dtype, int64_t t, int64_t ldx,
+                    const float* x_scales, int32_t x_group, void* y, int32_t y_dtype, int64_t ldy, void* work,
+                    int64_t work_bytes, void* stream) {
+  return product(w, nullptr, false, true, x, x_dtype, t, ldx, x_scales, x_group, y, y_dtype, ldy, work, work_bytes,
+                 stream);
+}
+
+int kashin_matmul_experts(const kashin_weights* w, const int64_t* offsets, int32_t transposed, const void* x,
+                          int32_t x_dtype, int64_t t, int64_t ldx, const float* x_scales, int32_t x_group, void* y,
+                          int32_t y_dtype, int64_t ldy, void* work, int64_t work_bytes, void* stream) {
+  if (transposed != 0 && transposed != 1) return fail(KASHIN_E_INVALID, "transposed must be 0 or 1");
+  return product(w, offsets, true, transposed != 0, x, x_dtype, t, ldx, x_scales, x_group, y, y_dtype, ldy, work,
+                 work_bytes, stream);
+}
+
 const char* kashin_status_string(int status) {
   switch (status) {
     case KASHIN_OK: return "ok";

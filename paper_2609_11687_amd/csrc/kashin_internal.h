@@ -198,4 +198,57 @@ bool rotate_supported_n(int n);
 hipError_t launch_rotate(int n, uint64_t seed, bool inverse, const void* x, int dtype, int64_t ldx, float* y,
                          int64_t ldy, int64_t m, hipStream_t stream);
 
+// RMS norm with the residual's addition (kashin_norm.hip); the fields are kashin_rmsnorm's arguments.
+struct NormArgs {
+  int64_t t;
+  int n;
+  const void* x;
+  int64_t ldx;
+  const void* r;
+  int64_t ldr;
+  const void* weight;
+  float eps;
+  void* h;
+  int64_t ldh;
+  void* y;
+  int y_dtype;
+  int64_t ldy;
+  float* scales;
+  int group;
+};
+constexpr int kNormMaxN = 16384;
+hipError_t launch_rmsnorm(const NormArgs& a, int dtype, hipStream_t stream);
+
+// Products from the codes (kashin_matmul.hip); the fields are kashin_matmul's arguments.
+struct ProductArgs {
+  KArgs p;  // the plan's operator tables, for P
+  int n;
+  int64_t m;
+  int groups;
+  int experts;
+  bool back;  // y = x W instead of x W^T
+  const uint8_t* codes_u;
+  const uint8_t* codes_v;
+  const float* centers;
+  const int64_t* offsets;  // null: all rows with the one matrix
+  bool rot;
+  uint64_t rot_seed;
+  const void* x;
+  int x_dtype;
+  int64_t t;
+  int64_t ldx;
+  const float* x_scales;
+  int x_group;
+  void* y;
+  int y_dtype;
+  int64_t ldy;
+  char* work;
+};
+constexpr int64_t kProductMaxRows = int64_t(1) << 16;  // t
+constexpr int64_t kProductMaxM = int64_t(1) << 24;
+constexpr int64_t kProductMaxK = int64_t(1) << 20;  // groups * n
+constexpr int kProductMaxExperts = 1024;
+int64_t product_workspace_bytes(int n, int64_t m, int groups, int64_t t, int experts, bool back);
+hipError_t launch_product(const ProductArgs& a, hipStream_t stream);
+
 }  // namespace kashin

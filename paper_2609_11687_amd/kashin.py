@@ -21,6 +21,7 @@ KASHIN_E_HIP = -4
 KASHIN_F32 = 0
 KASHIN_F16 = 1
 KASHIN_BF16 = 2
+KASHIN_E4M3 = 3
 
 EXPORTS = (
     "kashin_supported_n", "kashin_signs", "kashin_plan", "kashin_plan_destroy", "kashin_plan_signs",
@@ -28,7 +29,8 @@ EXPORTS = (
     "kashin_quantize", "kashin_quantize_grouped", "kashin_reconstruct_grouped", "kashin_apply_p", "kashin_rotate", "kashin_trace", "kashin_decompose_schedule",
     "kashin_trace_schedule", "kashin_quantize_rotated", "kashin_reconstruct_rotated", "kashin_optq_factor",
     "kashin_optq_workspace_bytes", "kashin_optq_quantize", "kashin_optq_quantize_noalloc", "kashin_status_string",
-    "kashin_last_error",
+    "kashin_last_error", "kashin_rmsnorm", "kashin_matmul", "kashin_matmul_t", "kashin_matmul_experts",
+    "kashin_matmul_workspace_bytes",
 )
 SCHEDULES = {"alternating": 0, "reverse": 1, "adaptive": 2, "original": 3}
 
@@ -74,12 +76,21 @@ def lib() -> ctypes.CDLL:
         "kashin_optq_quantize": [vp, vp, i64, i64, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp, i64, vp],
         "kashin_optq_quantize_noalloc": [vp, vp, i64, i64, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, vp, vp],
     }
+    f32, rows = ctypes.c_float, [vp, i32, i64, i64, vp, i32, vp, i32, i64, vp, i64, vp]
+    sig.update({
+        "kashin_rmsnorm": [i64, i32, vp, i32, i64, vp, i64, vp, f32, vp, i64, vp, i32, i64, vp, i32, vp],
+        "kashin_matmul": [vp] + rows,
+        "kashin_matmul_t": [vp] + rows,
+        "kashin_matmul_experts": [vp, vp, i32] + rows,
+    })
     for name, args in sig.items():
         fn = getattr(L, name)
         fn.argtypes = args
         fn.restype = ctypes.c_int
     L.kashin_optq_workspace_bytes.argtypes = [i64, i32, i32]
     L.kashin_optq_workspace_bytes.restype = i64
+    L.kashin_matmul_workspace_bytes.argtypes = [i32, i64, i32, i64, i32, i32]
+    L.kashin_matmul_workspace_bytes.restype = i64
     L.kashin_status_string.argtypes = [ctypes.c_int]
     L.kashin_status_string.restype = ctypes.c_char_p
     L.kashin_last_error.argtypes = []
@@ -469,6 +480,134 @@ def kashin_optq_quantize_noalloc(plan, w_t, u, v, chunk, exact, lloyd_iters, cod
                                               _ptr(centers), _ptr(q_t), _stream(stream)))
 
 
+# ----------------------------------------------------------------------------- a quantised model's layers
+def _float_codes():
+    import torch
+    return {torch.float32: KASHIN_F32, torch.float16: KASHIN_F16, torch.bfloat16: KASHIN_BF16}
+
+
+def _need_float_rows(t, name, device, width=None, rows=None, e4m3=False):
+    """(rows, leading dimension, dtype code) of a 2-D tensor with unit-stride rows on `device`."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    code = _float_codes().get(t.dtype)
+    if code is None and e4m3 and t.dtype == torch.float8_e4m3fn:
+        code = KASHIN_E4M3
+    if code is None:
+        raise TypeError(f"{name} has unsupported dtype {t.dtype}")
+    m, ld = _rows(t)
+    if (width is not None and t.shape[1] != width) or (rows is not None and m != rows):
+        raise ValueError(f"{name} must have shape {(rows if rows is not None else m, width)} (got {tuple(t.shape)})")
+    if m and (t.device.type != "cuda" or t.device != device):
+        raise ValueError(f"{name} must live on {device if device.type == 'cuda' else 'a cuda device'} (got {t.device})")
+    return m, ld, code
+
+
+def _stream_on(device, stream):
+    """`stream`, or the current one of `device` (a tensor's, which need not be the current device)."""
+    if stream is not None:
+        return _stream(stream)
+    import torch
+    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+
+
+def kashin_rmsnorm(x, residual, weight, eps, h, y, scales=None, group=0, stream=None):
+    """s = x + residual, h = s, y = s rsqrt(mean(s^2) + eps) weight row-wise; residual, weight and h may be None.
+    x, residual, weight, h: one dtype (fp32, fp16, bf16); y: fp32, fp16, bf16, or float8_e4m3fn with
+    scales (t x ceil(n / group) fp32, contiguous; t x 1 for group 0)."""
+    import torch
+    t, ldx, code = _need_float_rows(x, "x", x.device)
+    n = x.shape[1]
+    _, ldy, y_code = _need_float_rows(y, "y", x.device, n, t, e4m3=True)
+    ldr = ldh = n
+    for name, v in (("residual", residual), ("h", h), ("weight", weight)):
+        if v is not None and v.dtype != x.dtype:
+            raise TypeError(f"{name} must be {x.dtype} (got {v.dtype})")
+    if residual is not None:
+        _, ldr, _ = _need_float_rows(residual, "residual", x.device, n, t)
+    if h is not None:
+        _, ldh, _ = _need_float_rows(h, "h", x.device, n, t)
+    if weight is not None and (tuple(weight.shape) != (n,) or not weight.is_contiguous() or
+                               (t and weight.device != x.device)):
+        raise ValueError(f"weight must be {n} contiguous entries on {x.device}")
+    if scales is not None:
+        if group < 0:
+            raise ValueError("group must be >= 0")
+        _need(None, scales, (t, -(-n // group) if group else 1), torch.float32, "scales")
+        if t and scales.device != x.device:
+            raise ValueError(f"scales must live on {x.device}")
+    with torch.cuda.device(x.device if t else -1):
+        _check(lib().kashin_rmsnorm(t, n, _ptr(x), code, ldx, _ptr(residual), ldr, _ptr(weight), eps, _ptr(h), ldh,
+                                    _ptr(y), y_code, ldy, _ptr(scales), group,
+                                    _stream_on(x.device, stream) if t else None))
+
+
+class Weights(ctypes.Structure):
+    """kashin_weights of include/kashin.h."""
+    _fields_ = [("plan", ctypes.c_void_p), ("rot_seed", ctypes.c_void_p), ("codes_u", ctypes.c_void_p),
+                ("codes_v", ctypes.c_void_p), ("centers", ctypes.c_void_p), ("m", ctypes.c_int64),
+                ("groups", ctypes.c_int32), ("experts", ctypes.c_int32)]
+
+
+def kashin_matmul_workspace_bytes(n, m, groups, t, experts=1, transposed=False) -> int:
+    return int(lib().kashin_matmul_workspace_bytes(n, m, groups, t, experts, 1 if transposed else 0))
+
+
+def _matmul(name, plan, codes_u, codes_v, centers, x, y, work, x_scales, x_group, rot_seed, stream, transposed,
+            offsets=None):
+    import torch
+    wide, narrow = (y, x) if transposed else (x, y)  # k and m columns
+    if x.dim() != 2 or y.dim() != 2 or wide.shape[1] % plan.n or not wide.shape[1]:
+        raise ValueError(f"{'y' if transposed else 'x'} must have a multiple of {plan.n} columns "
+                         f"(got {tuple(wide.shape)})")
+    groups, m = wide.shape[1] // plan.n, narrow.shape[1]
+    experts = 1 if offsets is None else offsets.numel() - 1
+    device = torch.device("cuda", plan.device)
+    t, ldx, x_code = _need_float_rows(x, "x", device, e4m3=True)
+    _, ldy, y_code = _need_float_rows(y, "y", device, rows=t, width=y.shape[1])
+    _need_codes(plan, experts * m * groups, codes_u, codes_v, centers)
+    if offsets is not None:
+        _need(plan, offsets, (experts + 1,), torch.int64, "offsets")
+    if x_scales is not None:
+        if x_group < 0:
+            raise ValueError("x_group must be >= 0")
+        _need(plan, x_scales, (t, -(-x.shape[1] // x_group) if x_group else 1), torch.float32, "x_scales")
+    if work.dtype != torch.uint8 or work.dim() != 1 or (work.numel() and not work.is_contiguous()):
+        raise ValueError("work must be a contiguous 1-D uint8 tensor")
+    if work.numel():
+        _on_plan_device(plan, work, "work")
+    seed = None if rot_seed is None else ctypes.c_uint64(rot_seed)
+    w = Weights(plan.handle, None if seed is None else ctypes.addressof(seed), codes_u.data_ptr(), codes_v.data_ptr(),
+                centers.data_ptr(), m, groups, experts)
+    more = () if offsets is None else (_ptr(offsets), 1 if transposed else 0)
+    _check(getattr(lib(), name)(ctypes.addressof(w), *more, _ptr(x), x_code, t, ldx, _ptr(x_scales), x_group, _ptr(y),
+                                y_code, ldy, _ptr(work), work.numel(), _stream_on(device, stream) if t else None))
+
+
+def kashin_matmul(plan, codes_u, codes_v, centers, x, y, work, x_scales=None, x_group=0, rot_seed=None, stream=None):
+    """y = x W^T for W (m x k) held as codes and centres of m * groups rows (k = groups * plan.n, as quantised from
+    W.view(m * groups, plan.n)); x (t x k) fp32, fp16, bf16, or float8_e4m3fn with x_scales (t x ceil(k / x_group), t x 1
+    for x_group 0); y (t x m) fp32, fp16 or bf16; work: a uint8 buffer of at least kashin_matmul_workspace_bytes."""
+    _matmul("kashin_matmul", plan, codes_u, codes_v, centers, x, y, work, x_scales, x_group, rot_seed, stream, False)
+
+
+def kashin_matmul_t(plan, codes_u, codes_v, centers, x, y, work, x_scales=None, x_group=0, rot_seed=None, stream=None):
+    """y = x W (x t x m, y t x k): the product for codes held transposed (kashin_optq_quantize's), and the gradient of
+    kashin_matmul with respect to its x."""
+    _matmul("kashin_matmul_t", plan, codes_u, codes_v, centers, x, y, work, x_scales, x_group, rot_seed, stream, True)
+
+
+def kashin_matmul_experts(plan, codes_u, codes_v, centers, offsets, x, y, work, transposed=False, x_scales=None, x_group=0,
+                          rot_seed=None, stream=None):
+    """kashin_matmul (or kashin_matmul_t) grouped by expert: rows offsets[e] .. offsets[e + 1] - 1 with expert e's matrix
+    (codes and centres of all experts, one behind the other); offsets: experts + 1 int64 on the device, not decreasing."""
+    if offsets.dim() != 1 or offsets.numel() < 2:
+        raise ValueError("offsets must hold one more entry than there are experts")
+    _matmul("kashin_matmul_experts", plan, codes_u, codes_v, centers, x, y, work, x_scales, x_group, rot_seed, stream,
+            bool(transposed), offsets)
+
+
 # ----------------------------------------------------------------------------- allocating helpers
 def quantize_alloc(plan, w, lloyd_iters=0, stream=None):
     """Allocate outputs (torch, on w's device) and run kashin_quantize."""
@@ -493,3 +632,21 @@ def decompose_alloc(plan, w, want_r=False, stream=None):
     bd = torch.empty((m, 4), **f)
     kashin_decompose(plan, w, u, vh, r, cs, bd, stream)
     return u, vh, r, cs, bd
+
+
+def matmul_alloc(plan, codes_u, codes_v, centers, x, groups=1, transposed=False, out_dtype=None, x_scales=None, x_group=0,
+                 rot_seed=None, stream=None):
+    """Allocate the output (out_dtype; x's dtype by default) and the workspace (torch, on x's device) and run
+    kashin_matmul, or kashin_matmul_t; on `stream` (a torch stream) the buffers are that stream's too."""
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return matmul_alloc(plan, codes_u, codes_v, centers, x, groups, transposed, out_dtype, x_scales, x_group,
+                                rot_seed)
+    m, t = codes_u.shape[0] // groups, x.shape[0]
+    y = torch.empty((t, groups * plan.n if transposed else m), dtype=out_dtype or x.dtype, device=x.device)
+    work = torch.empty(kashin_matmul_workspace_bytes(plan.n, m, groups, t, 1, transposed), dtype=torch.uint8,
+                       device=x.device)
+    (kashin_matmul_t if transposed else kashin_matmul)(plan, codes_u, codes_v, centers, x, y, work, x_scales, x_group,
+                                                      rot_seed)
+    return y

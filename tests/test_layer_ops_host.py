@@ -1,0 +1,99 @@
+"""Host-side checks of the operators of a quantised model's layers: refusals before any device is touched."""
+import ctypes
+
+import pytest
+
+from paper_2609_11687_amd import kashin as K
+
+X, Y, R, H, S, W = (0x100000 * i for i in range(1, 7))
+
+
+def _norm(t=4, n=512, x=X, dtype=0, ldx=512, r=None, ldr=512, weight=None, eps=1e-5, h=None, ldh=512, y=Y, y_dtype=0, ldy=512,
+          scales=None, group=0):
+    return K.lib().kashin_rmsnorm(t, n, x, dtype, ldx, r, ldr, weight, eps, h, ldh, y, y_dtype, ldy, scales, group, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    ({"n": 0}, K.KASHIN_E_UNSUPPORTED_N), ({"n": 16385, "ldx": 20000, "ldy": 20000}, K.KASHIN_E_UNSUPPORTED_N),
+    ({"t": -1}, K.KASHIN_E_INVALID), ({"dtype": 3}, K.KASHIN_E_INVALID), ({"dtype": -1}, K.KASHIN_E_INVALID),
+    ({"y_dtype": 4}, K.KASHIN_E_INVALID), ({"eps": -1.0}, K.KASHIN_E_INVALID), ({"eps": float("nan")}, K.KASHIN_E_INVALID),
+    ({"eps": float("inf")}, K.KASHIN_E_INVALID), ({"ldx": 511}, K.KASHIN_E_INVALID), ({"ldy": 511}, K.KASHIN_E_INVALID),
+    ({"r": R, "ldr": 511}, K.KASHIN_E_INVALID), ({"h": H, "ldh": 511}, K.KASHIN_E_INVALID),
+    ({"y_dtype": 3, "scales": S, "group": 48}, K.KASHIN_E_INVALID), ({"y_dtype": 3, "scales": S, "group": -32}, K.KASHIN_E_INVALID),
+    ({"y_dtype": 3}, K.KASHIN_E_INVALID), ({"scales": S}, K.KASHIN_E_INVALID), ({"group": 128}, K.KASHIN_E_INVALID),
+    ({"x": None}, K.KASHIN_E_INVALID), ({"y": None}, K.KASHIN_E_INVALID), ({"y": X}, K.KASHIN_E_INVALID),
+    ({"y": X + 4 * (3 * 512 + 511)}, K.KASHIN_E_INVALID), ({"h": X + 4}, K.KASHIN_E_INVALID),
+    ({"h": X, "ldh": 600}, K.KASHIN_E_INVALID), ({"r": R, "h": R + 2048}, K.KASHIN_E_INVALID), ({"r": Y}, K.KASHIN_E_INVALID),
+    ({"weight": Y + 64}, K.KASHIN_E_INVALID), ({"h": H, "weight": H}, K.KASHIN_E_INVALID), ({"h": Y}, K.KASHIN_E_INVALID),
+    ({"y_dtype": 3, "scales": X, "group": 0}, K.KASHIN_E_INVALID), ({"y_dtype": 3, "scales": Y + 8}, K.KASHIN_E_INVALID),
+    ({"t": 0, "x": None, "y": None}, K.KASHIN_OK),
+])
+def test_rmsnorm_refusals(kw, status):
+    assert _norm(**kw) == status
+    assert bool(K.lib().kashin_last_error()) == (status != K.KASHIN_OK)
+
+
+def test_product_entry_points_reject_dead_plans():
+    L = K.lib()
+    args = (X, 0, 2, 512, None, 0, Y, 0, 4, W, 1 << 20, None)
+    for plan in (None, 0x1234):
+        w = K.Weights(plan, None, X, X, X, 4, 1, 1)
+        assert L.kashin_matmul(ctypes.addressof(w), *args) == K.KASHIN_E_INVALID
+        assert "plan" in L.kashin_last_error().decode()
+        assert L.kashin_matmul_t(ctypes.addressof(w), *args) == K.KASHIN_E_INVALID
+        assert L.kashin_matmul_experts(ctypes.addressof(w), X, 0, *args) == K.KASHIN_E_INVALID
+        assert "plan" in L.kashin_last_error().decode()
+    assert L.kashin_matmul(None, *args) == K.KASHIN_E_INVALID
+    assert L.kashin_matmul_experts(None, X, 0, *args) == K.KASHIN_E_INVALID
+    assert L.kashin_matmul_experts(None, X, 5, *args) == K.KASHIN_E_INVALID
+    assert ctypes.sizeof(K.Weights) == 56
+
+
+@pytest.mark.parametrize("args", [(100, 4, 1, 1, 1, 0), (512, 0, 1, 1, 1, 0), (512, (1 << 24) + 1, 1, 1, 1, 0), (512, 4, 0, 1, 1, 0),
+                                  (512, 4, (1 << 20) // 512 + 1, 1, 1, 0), (512, 4, 1, -1, 1, 0), (512, 4, 1, (1 << 16) + 1, 1, 0),
+                                  (512, 4, 1, 1, 0, 0), (512, 4, 1, 1, 1025, 0), (512, 4, 1, 1, 1, 2)])
+def test_workspace_sizes_refused(args):
+    assert K.lib().kashin_matmul_workspace_bytes(*args) == -1
+
+
+def test_workspace_sizes_grow_with_the_rows():
+    for back in (False, True):
+        sizes = [K.kashin_matmul_workspace_bytes(4096, 11008, 1, t, 1, back) for t in (0, 1, 2, 17, 300, 4000, 65536)]
+        assert sizes[0] >= 0 and sizes == sorted(sizes)
+        assert K.kashin_matmul_workspace_bytes(4096, 11008, 1, 300, 8, back) >= sizes[4]
+
+
+def test_binding_checks_before_calling():
+    import torch
+
+    plan = K.Plan(None, 512, 0, 4, 0)
+    z = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype)  # noqa: E731
+    codes = z(0, 128, dtype=torch.uint8), z(0, 128, dtype=torch.uint8), z(0, 2, 4)
+    work = z(0, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="columns"):
+        K.kashin_matmul(plan, *codes, z(0, 500), z(0, 4), work)
+    with pytest.raises(ValueError, match="columns"):
+        K.kashin_matmul_t(plan, *codes, z(0, 4), z(0, 500), work)
+    with pytest.raises(ValueError, match="shape"):
+        K.kashin_matmul(plan, *codes, z(0, 512), z(0, 4), work)  # codes of four rows are needed
+    with pytest.raises(TypeError, match="dtype"):
+        K.kashin_matmul(plan, *codes, z(0, 512, dtype=torch.float64), z(0, 4), work)
+    with pytest.raises(TypeError, match="dtype"):
+        K.kashin_matmul(plan, *codes, z(0, 512), z(0, 4, dtype=torch.int32), work)
+    with pytest.raises(ValueError, match="cuda"):
+        K.kashin_matmul(plan, *codes, z(2, 512), z(2, 4), work)
+    with pytest.raises(ValueError, match="offsets"):
+        K.kashin_matmul_experts(plan, *codes, z(1, dtype=torch.int64), z(0, 512), z(0, 4), work)
+    with pytest.raises(TypeError, match="offsets"):
+        K.kashin_matmul_experts(plan, *codes, z(2, dtype=torch.int32), z(0, 512), z(0, 0), work)
+    with pytest.raises(ValueError, match="shape"):
+        K.kashin_rmsnorm(z(0, 64), None, None, 1e-5, None, z(0, 63))
+    with pytest.raises(TypeError, match="residual"):
+        K.kashin_rmsnorm(z(0, 64), z(0, 64, dtype=torch.float16), None, 1e-5, None, z(0, 64))
+    with pytest.raises(ValueError, match="weight"):
+        K.kashin_rmsnorm(z(0, 64), None, z(63), 1e-5, None, z(0, 64))
+    with pytest.raises(ValueError, match="shape"):
+        K.kashin_rmsnorm(z(0, 64), None, None, 1e-5, None, z(0, 64, dtype=torch.float8_e4m3fn), z(0, 1), 32)
+    with pytest.raises(K.KashinError):
+        K.kashin_rmsnorm(z(0, 64), None, None, 1e-5, None, z(0, 64), None, 32)
+    K.kashin_rmsnorm(z(0, 64), None, None, 1e-5, None, z(0, 64))  # no rows: nothing to do
