@@ -91,37 +91,293 @@ __device__ __forceinline__ void put(void* y, int dtype, int64_t i, float v) {
   else static_cast<__bf16*>(y)[i] = static_cast<__bf16>(v);
 }
 
-// y[t][i] = sum_k u[i][k] x[t][k] + v[i][k] px[t][k]: a wave for each matrix row and tile of four rows.
-constexpr int kTT = 4;
-__global__ __launch_bounds__(64) void rows_kernel(ProductArgs a, const float* x, const float* px) {
-  const Tile tl = find_tile<kTT>(a.offsets, a.experts, a.t, blockIdx.y);
+// ------------------------------------------------------------------ operands of the matrix instructions
+// Products run on fp16 matrix instructions with fp32 sums.  fp32 operands are two fp16 parts, hi + lo, which hold 22
+// bits: x y = hi hi + hi lo + lo hi to 2^-21.  Both operands are scaled by powers of two first, a row of x with P x and a
+// matrix row's centres each by its largest magnitude, into fp16's range.
+using half8 = _Float16 __attribute__((ext_vector_type(8)));
+using float4_t = float __attribute__((ext_vector_type(4)));
+using uint4_t = uint32_t __attribute__((ext_vector_type(4)));
+
+constexpr int kChunk = 64;  // codes a lane decodes from one 16-byte load
+constexpr int kUnits = 8;   // units of 8 codes in a chunk: one operand register block of a matrix instruction each
+constexpr int kSlab = 4;    // chunks that the four quarters of a wave work on side by side
+
+__host__ __device__ inline int chunks_per_group(int n) { return (n + kChunk - 1) / kChunk; }
+// chunks of a factor, to a multiple of the slab (the last ones may be empty)
+__host__ __device__ inline int64_t padded_chunks(int n, int groups) {
+  return (static_cast<int64_t>(groups) * chunks_per_group(n) + kSlab - 1) / kSlab * kSlab;
+}
+
+// Entry k of a unit's eight: units 2d and 2d + 1 of a chunk come from its dword d, whose 16 codes leave four at a time, two
+// bits of every byte.
+__device__ constexpr int unit_entry(int unit, int k) { return 16 * (unit / 2) + 2 * (unit % 2) + k / 4 + 4 * (k % 4); }
+
+// Exponent s that takes a largest magnitude (as bits) into [2^13, 2^14) when multiplied by 2^s; NaN or infinity: none.
+__device__ __forceinline__ int scale_exponent(uint32_t top) {
+  const int e = 267 - static_cast<int>(top >> 23);
+  return (e > 253 ? 253 : e) - 127;
+}
+__device__ __forceinline__ float power_of_two(int s) { return __uint_as_float(static_cast<uint32_t>(s + 127) << 23); }
+constexpr uint32_t kInfBits = 0x7f800000u;
+
+// The four centres of a factor as fp16 hi and lo parts, split into their low and high bytes: an entry of a table of
+// four 16-bit values is two byte selections.
+struct Table {
+  uint32_t hi0, hi1, lo0, lo1;
+};
+__device__ __forceinline__ uint32_t pair_bits(_Float16 a, _Float16 b) {
+  return static_cast<uint32_t>(__builtin_bit_cast(uint16_t, a)) |
+         (static_cast<uint32_t>(__builtin_bit_cast(uint16_t, b)) << 16);
+}
+__device__ __forceinline__ Table make_table(float4_t q, float scale) {
+  _Float16 h[4], l[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const float v = q[c] * scale;
+    h[c] = static_cast<_Float16>(v);
+    l[c] = static_cast<_Float16>(v - static_cast<float>(h[c]));
+  }
+  const uint32_t a = pair_bits(h[0], h[1]), b = pair_bits(h[2], h[3]), c = pair_bits(l[0], l[1]), d = pair_bits(l[2], l[3]);
+  return {__builtin_amdgcn_perm(b, a, 0x06040200u), __builtin_amdgcn_perm(b, a, 0x07050301u),
+          __builtin_amdgcn_perm(d, c, 0x06040200u), __builtin_amdgcn_perm(d, c, 0x07050301u)};
+}
+
+// Eight values of unit `h` (0, 1) of a dword of 16 codes, hi and (LO) lo parts.
+template <bool LO>
+__device__ __forceinline__ void decode8(uint32_t w, int h, const Table& tb, half8& hi, half8& lo) {
+  uint4_t a, b;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t c = (w >> (4 * h + 2 * k)) & 0x03030303u;
+    uint32_t l = __builtin_amdgcn_perm(0, tb.hi0, c), u = __builtin_amdgcn_perm(0, tb.hi1, c);
+    a[2 * k] = __builtin_amdgcn_perm(u, l, 0x05010400u);
+    a[2 * k + 1] = __builtin_amdgcn_perm(u, l, 0x07030602u);
+    if constexpr (LO) {
+      l = __builtin_amdgcn_perm(0, tb.lo0, c);
+      u = __builtin_amdgcn_perm(0, tb.lo1, c);
+      b[2 * k] = __builtin_amdgcn_perm(u, l, 0x05010400u);
+      b[2 * k + 1] = __builtin_amdgcn_perm(u, l, 0x07030602u);
+    }
+  }
+  hi = __builtin_bit_cast(half8, a);
+  if constexpr (LO) lo = __builtin_bit_cast(half8, b);
+}
+
+// A chunk's 16 bytes of codes.  The last chunk of a group may be short (n no multiple of 64): then the group's
+// last 16 bytes are read (n >= 64) and moved down; what follows its codes meets zeros of x.
+__device__ __forceinline__ uint4_t load_codes(const uint8_t* group, int nby, int off) {
+  const int left = nby - off;
+  uint4_t v;
+  if (left >= 16) {
+    __builtin_memcpy(&v, group + off, 16);
+    return v;
+  }
+  uint64_t q[2];
+  __builtin_memcpy(q, group + nby - 16, 16);
+  const int bits = 8 * (16 - left);  // 8 .. 120
+  if (bits >= 64) {
+    q[0] = q[1] >> (bits - 64);
+    q[1] = 0;
+  } else {
+    q[0] = (q[0] >> bits) | (q[1] << (64 - bits));
+    q[1] >>= bits;
+  }
+  __builtin_memcpy(&v, q, 16);
+  return v;
+}
+
+// ------------------------------------------------------------------ x W^T: x and P x as operands
+// frags[part][factor][unit][row][8]: hi (part 0) and lo parts of scaled x (factor 0) and P x, eight entries of a row
+// in the order of a unit's codes; rows innermost, so that the lanes of a matrix instruction's operand read consecutive 16
+// bytes.  exps[row]: the exponent of the scale.  One workgroup a row.
+constexpr int kSplitT = 512;
+__global__ __launch_bounds__(kSplitT) void split_rows_kernel(const float* x, const float* px, int n, int groups, int64_t t,
+                                                             bool lo, _Float16* frags, int32_t* exps) {
+  __shared__ uint32_t part[kSplitT / 64];
+  const int64_t row = blockIdx.x, k = static_cast<int64_t>(groups) * n;
+  const float* src[2] = {x + row * k, px + row * k};
+  uint32_t top = 0;
+  for (int f = 0; f < 2; ++f)
+    for (int64_t i = threadIdx.x * 4; i < k; i += kSplitT * 4) {  // n is a multiple of 4
+      const float4_t v = *reinterpret_cast<const float4_t*>(src[f] + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
+        top = b > top ? b : top;
+      }
+    }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_xor(top, d);
+    top = o > top ? o : top;
+  }
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSplitT / 64; ++w) top = part[w] > top ? part[w] : top;
+  const bool bad = top >= kInfBits;
+  const int e = bad ? 0 : scale_exponent(top);
+  const float scale = bad ? __int_as_float(0x7fc00000) : power_of_two(e);
+  if (threadIdx.x == 0) exps[row] = e;
+  const int cpg = chunks_per_group(n);
+  const int64_t units = padded_chunks(n, groups) * kUnits, real = static_cast<int64_t>(groups) * cpg * kUnits;
+  for (int64_t u = threadIdx.x; u < 2 * units; u += kSplitT) {
+    const int f = u >= units;
+    const int64_t un = u - f * units;
+    half8 h = {}, l = {};
+    if (un < real) {
+      const int g = static_cast<int>(un / (cpg * kUnits)), in_group = static_cast<int>(un % (cpg * kUnits));
+      const int base = in_group / kUnits * kChunk, unit = in_group % kUnits;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int at = base + unit_entry(unit, j);
+        const float v = at < n ? src[f][static_cast<int64_t>(g) * n + at] * scale : 0.f;
+        h[j] = static_cast<_Float16>(v);
+        l[j] = static_cast<_Float16>(v - static_cast<float>(h[j]));
+      }
+    }
+    *reinterpret_cast<half8*>(frags + (u * t + row) * 8) = h;
+    if (lo) *reinterpret_cast<half8*>(frags + ((u + 2 * units) * t + row) * 8) = l;
+  }
+}
+
+// y = x W^T for few rows of x: a workgroup computes 16 R matrix rows for a tile of rows of x, its eight waves taking an
+// eighth of the codes each and their sums joined through LDS in a fixed order.  Operand A: lane (r, q) decodes chunk
+// 4 s + q of matrix row r, operand B: the same chunk's entries of x's rows.  J tiles of 16 rows of x, or J = 0: 8
+// rows, whose hi parts are B's columns 0 .. 7 and lo parts columns 8 .. 15, so that two instructions give all four products
+// (against three for 16 rows).
+constexpr int kRowsT = 512;
+template <int J>
+constexpr int tile_rows() { return J == 0 ? 8 : 16 * J; }
+
+template <int J, int R>
+__global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _Float16* frags, const int32_t* exps) {
+  constexpr int TT = tile_rows<J>(), JJ = J == 0 ? 1 : J, NW = kRowsT / 64, RP = 16 * R + 4;
+  __shared__ float sums[NW][16 * JJ][RP];
+  __shared__ uint32_t tops[16 * R];
+  const Tile tl = find_tile<TT>(a.offsets, a.experts, a.t, blockIdx.y);
   if (tl.rows == 0) return;
-  const int n = a.n, nby = n / 4, lane = threadIdx.x;
-  const int64_t k = static_cast<int64_t>(a.groups) * n, i = blockIdx.x;
-  float acc[kTT] = {};
-  for (int g = 0; g < a.groups; ++g) {
-    const int64_t row = (tl.expert * a.m + i) * a.groups + g;
-    const float* q = a.centers + row * 8;
-    for (int b = lane; b < nby; b += 64) {
-      const int cu = a.codes_u[row * nby + b], cv = a.codes_v[row * nby + b];
+  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int r = lane % 16, q = lane / 16, cpg = chunks_per_group(n);
+  const int chunks = a.groups * cpg;
+  const int slabs = static_cast<int>(padded_chunks(n, a.groups) / kSlab);
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * (16 * R);
+  // matrix rows past the last repeat it
+  int64_t first[R];  // this lane's rows, as the first of their groups' rows of codes
 #pragma unroll
-      for (int s = 0; s < kTT; ++s) {
-        if (s >= tl.rows) break;
-        const int64_t at = (tl.row0 + s) * k + g * n + 4 * b;
+  for (int i = 0; i < R; ++i) {
+    const int64_t row = row0 + 16 * i + r;
+    first[i] = (tl.expert * a.m + (row < a.m ? row : a.m - 1)) * a.groups;
+  }
+  // this wave's items: item = factor * slabs + slab
+  const int items = 2 * slabs, i0 = items * wave / NW, i1 = items * (wave + 1) / NW;
+  constexpr int AHEAD = 3;
+  uint4_t codes[AHEAD][R];
+  auto load_item = [&](int it, uint4_t (&c)[R]) {
+    const int f = it >= slabs, chunk = (it - f * slabs) * kSlab + q;
+    const uint8_t* base = f ? a.codes_v : a.codes_u;
+    const int at = chunk < chunks ? chunk : chunks - 1;
+    const int g = a.groups == 1 ? 0 : at / cpg, off = (at - g * cpg) * 16;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc[s] += pick(q, (cu >> (2 * j)) & 3) * x[at + j] + pick(q + 4, (cv >> (2 * j)) & 3) * px[at + j];
+    for (int i = 0; i < R; ++i) c[i] = load_codes(base + (first[i] + g) * nby, nby, off);
+  };
+#pragma unroll
+  for (int d = 0; d < AHEAD; ++d)
+    if (i0 + d < i1) load_item(i0 + d, codes[d]);
+  // the scale of every matrix row: its largest centre over all groups
+  if (tid < 16 * R) tops[tid] = 0;
+  __syncthreads();
+  {
+    uint32_t top = 0;
+    const int mine = tid % (16 * R);
+    const int64_t row = row0 + mine;
+    const float* ce = a.centers + (tl.expert * a.m + (row < a.m ? row : a.m - 1)) * a.groups * 8;
+    for (int64_t j = tid / (16 * R); j < a.groups * 8; j += kRowsT / (16 * R)) {
+      const uint32_t b = __float_as_uint(ce[j]) & 0x7fffffffu;
+      top = b > top ? b : top;
+    }
+    if (top) atomicMax(&tops[mine], top);  // a maximum: the same in any order
+  }
+  __syncthreads();
+  float scale[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const uint32_t top = tops[16 * i + r];
+    scale[i] = top >= kInfBits ? __int_as_float(0x7fc00000) : power_of_two(scale_exponent(top));
+  }
+  // B: column c of tile j is row 16 j + c of the tile (J = 0: row c % 8, hi or lo part); columns past the last repeat it
+  const int64_t units = static_cast<int64_t>(slabs) * kSlab * kUnits;
+  const _Float16* col[JJ];
+#pragma unroll
+  for (int j = 0; j < JJ; ++j) {
+    int c = J == 0 ? r % 8 : 16 * j + r;
+    c = c < tl.rows ? c : tl.rows - 1;
+    col[j] = frags + (tl.row0 + c) * 8 + (J == 0 && r >= 8 ? 2 * units * a.t * 8 : 0);
+  }
+  float4_t acc[JJ][R];
+#pragma unroll
+  for (int j = 0; j < JJ; ++j)
+#pragma unroll
+    for (int i = 0; i < R; ++i) acc[j][i] = float4_t{0.f, 0.f, 0.f, 0.f};
+  Table tb[R];
+  int held = -1;  // the (factor, group) whose tables tb holds
+  for (int b0 = i0; b0 < i1; b0 += AHEAD) {
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) {
+      const int it = b0 + d;
+      if (it >= i1) break;
+      const int f = it >= slabs, chunk = (it - f * slabs) * kSlab + q;
+      const int g = a.groups == 1 ? 0 : (chunk < chunks ? chunk : chunks - 1) / cpg;
+      const int64_t unit0 = f * units + static_cast<int64_t>(chunk) * kUnits;
+      if (f * a.groups + g != held) {
+        held = f * a.groups + g;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+          tb[i] = make_table(*reinterpret_cast<const float4_t*>(a.centers + (first[i] + g) * 8 + 4 * f), scale[i]);
+      }
+      uint4_t now[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) now[i] = codes[d][i];
+      if (it + AHEAD < i1) load_item(it + AHEAD, codes[d]);
+#pragma unroll
+      for (int s = 0; s < kUnits; ++s) {
+        half8 hi[R], lo[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) decode8<true>(now[i][s / 2], s % 2, tb[i], hi[i], lo[i]);
+#pragma unroll
+        for (int j = 0; j < JJ; ++j) {
+          const half8 xh = *reinterpret_cast<const half8*>(col[j] + (unit0 + s) * a.t * 8);
+          half8 xl = {};
+          if constexpr (J != 0) xl = *reinterpret_cast<const half8*>(col[j] + (unit0 + s + 2 * units) * a.t * 8);
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[i], xh, acc[j][i], 0, 0, 0);
+            if constexpr (J != 0) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[i], xl, acc[j][i], 0, 0, 0);
+            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[i], xh, acc[j][i], 0, 0, 0);
+          }
+        }
       }
     }
   }
 #pragma unroll
-  for (int s = 0; s < kTT; ++s) {
+  for (int j = 0; j < JJ; ++j)
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) acc[s] += __shfl_xor(acc[s], d);
-    if (lane == 0 && s < tl.rows) put(a.y, a.y_dtype, (tl.row0 + s) * a.ldy + i, acc[s]);
+    for (int i = 0; i < R; ++i) *reinterpret_cast<float4_t*>(&sums[wave][16 * j + r][16 * i + 4 * q]) = acc[j][i];
+  __syncthreads();
+  for (int o = tid; o < TT * 16 * R; o += kRowsT) {
+    const int c = o / (16 * R), i = o % (16 * R);
+    if (c >= tl.rows || row0 + i >= a.m) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) v += J == 0 ? sums[w][c][i] + sums[w][c + 8][i] : sums[w][c][i];
+    const uint32_t top = tops[i];
+    const int e = top >= kInfBits ? 0 : scale_exponent(top);
+    put(a.y, a.y_dtype, (tl.row0 + c) * a.ldy + row0 + i, ldexpf(v, -(e + exps[tl.row0 + c])));
   }
 }
 
+constexpr int kTT = 4;
 // zu[t][j] = sum_i x[t][i] u[i][j], zv alike: a thread for each byte of codes (four columns).
 __global__ __launch_bounds__(64) void columns_kernel(ProductArgs a, const float* x, float* zu, float* zv) {
   const Tile tl = find_tile<kTT>(a.offsets, a.experts, a.t, blockIdx.y);
@@ -214,12 +470,21 @@ hipError_t rotate(const ProductArgs& a, bool inverse, float* z, hipStream_t s) {
   return launch_rotate(a.n, a.rot_seed, inverse, z, KASHIN_F32, a.n, z, a.n, a.t * a.groups, s);
 }
 
+template <int J, int R>
+hipError_t launch_rows(const ProductArgs& a, const _Float16* frags, const int32_t* exps, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>((a.m + 16 * R - 1) / (16 * R)),
+                  static_cast<unsigned>(most_tiles(a, tile_rows<J>())));
+  hipLaunchKernelGGL((rows_kernel<J, R>), grid, dim3(kRowsT), 0, s, a, frags, exps);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 int64_t product_workspace_bytes(int n, int64_t m, int groups, int64_t t, int experts, bool back) {
   (void)experts;
   const int64_t k = static_cast<int64_t>(groups) * n;
-  return align256(t * (back ? m : k) * 4) + (back ? 3 : 1) * align256(t * k * 4);
+  if (back) return align256(t * m * 4) + 3 * align256(t * k * 4);
+  return 2 * align256(t * k * 4) + align256(t * 4) + 4 * padded_chunks(n, groups) * kUnits * t * 16;
 }
 
 hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
@@ -227,22 +492,31 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
   float* x = reinterpret_cast<float*>(a.work);
   float* z[3];
   for (int i = 0; i < 3; ++i) z[i] = reinterpret_cast<float*>(a.work + align256(a.t * wx * 4) + i * align256(a.t * k * 4));
-  const unsigned tiles = static_cast<unsigned>(most_tiles(a, kTT)), t = static_cast<unsigned>(a.t);
+  const unsigned t = static_cast<unsigned>(a.t);
   hipError_t e = widen(a, wx, x, s);
   if (e != hipSuccess) return e;
   if (!a.back) {
     if (a.rot) e = rotate(a, false, x, s);
     if (e == hipSuccess) e = apply_p(a, x, z[0], s);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(rows_kernel, dim3(static_cast<unsigned>(a.m), tiles), dim3(64), 0, s, a, x, z[0]);
-    return hipGetLastError();
+    int32_t* exps = reinterpret_cast<int32_t*>(a.work + 2 * align256(a.t * k * 4));
+    _Float16* frags = reinterpret_cast<_Float16*>(a.work + 2 * align256(a.t * k * 4) + align256(a.t * 4));
+    hipLaunchKernelGGL(split_rows_kernel, dim3(t), dim3(kSplitT), 0, s, x, z[0], a.n, a.groups, a.t, true, frags, exps);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t each = a.offsets == nullptr ? a.t : a.t / (a.experts < a.t ? a.experts : a.t);
+    if (each <= 8) return launch_rows<0, 1>(a, frags, exps, s);
+    if (each <= 16) return launch_rows<1, 1>(a, frags, exps, s);
+    if (each <= 32) return launch_rows<2, 2>(a, frags, exps, s);
+    return launch_rows<4, 2>(a, frags, exps, s);
   }
   const dim3 whole(t, static_cast<unsigned>((k + 255) / 256));
   if (a.offsets != nullptr) {
     hipLaunchKernelGGL(clear_spare_kernel, whole, dim3(256), 0, s, a.offsets, a.experts, k, z[1]);
     hipLaunchKernelGGL(clear_spare_kernel, whole, dim3(256), 0, s, a.offsets, a.experts, k, z[0]);
   }
-  hipLaunchKernelGGL(columns_kernel, dim3(static_cast<unsigned>((k / 4 + 63) / 64), tiles), dim3(64), 0, s, a, x, z[0], z[1]);
+  hipLaunchKernelGGL(columns_kernel, dim3(static_cast<unsigned>((k / 4 + 63) / 64), static_cast<unsigned>(most_tiles(a, kTT))),
+                     dim3(64), 0, s, a, x, z[0], z[1]);
   e = hipGetLastError();
   if (e == hipSuccess) e = apply_p(a, z[1], z[2], s);
   if (e != hipSuccess) return e;
