@@ -60,9 +60,9 @@ __device__ Tile find_tile(const int64_t* offsets, int experts, int64_t t, int ti
   return r;
 }
 // The most tiles that offsets in order can give: whole ones, and a partial one for each expert with rows.
-int64_t most_tiles(const ProductArgs& a, int64_t tt) {
-  if (a.offsets == nullptr) return (a.t + tt - 1) / tt;
-  return a.t / tt + (a.experts < a.t ? a.experts : a.t);
+int64_t most_tiles(bool grouped, int64_t t, int experts, int64_t tt) {
+  if (!grouped) return (t + tt - 1) / tt;
+  return t / tt + (experts < t ? experts : t);
 }
 
 // x as contiguous fp32 rows.
@@ -377,39 +377,245 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
   }
 }
 
-constexpr int kTT = 4;
-// zu[t][j] = sum_i x[t][i] u[i][j], zv alike: a thread for each byte of codes (four columns).
-__global__ __launch_bounds__(64) void columns_kernel(ProductArgs a, const float* x, float* zu, float* zv) {
-  const Tile tl = find_tile<kTT>(a.offsets, a.experts, a.t, blockIdx.y);
-  if (tl.rows == 0) return;
-  const int n = a.n, nby = n / 4;
-  const int64_t k = static_cast<int64_t>(a.groups) * n;
-  const int64_t col = static_cast<int64_t>(blockIdx.x) * 64 + threadIdx.x;  // byte of the row of all groups
-  if (col >= k / 4) return;
-  const int g = static_cast<int>(col / nby), b = static_cast<int>(col % nby);
-  float au[kTT][4] = {}, av[kTT][4] = {};
-  for (int64_t i = 0; i < a.m; ++i) {
-    const int64_t row = (tl.expert * a.m + i) * a.groups + g;
-    const float* q = a.centers + row * 8;
-    const int cu = a.codes_u[row * nby + b], cv = a.codes_v[row * nby + b];
+// ------------------------------------------------------------------ x W: the columns of the codes
+// y[t][c] = sum_i x[t][i] w[i][c]: the sum runs over matrix rows, whose centres differ, while a lane of operand A holds
+// one column of eight rows.  A row's four centres q are therefore taken apart into functions of the code that
+// A can hold without a table,
+//   q[code] = a + p0 b0 + p1 b1 + d f,   b0 = {0,1,0,1}, b1 = {0,0,2,2}, f = {0,1,2,4},
+//   a = q0, d = q3 - q2 - q1 + q0, p0 = q1 - q0 - d, p1 = (q2 - q0) / 2 - d,
+// and the coefficients times x go into operand B (two fp16 parts).  With a code's two bits at bits 10 and 11 of a
+// 16-bit half, the halves masked by 0x0400, 0x0800 and 0x0c00 are the fp16 numbers b0, b1 and f times 2^-14: two codes
+// take a shift and three ands.
+//
+// Exponents of x's rows and the largest finite centres: x goes to fp32 with max |x| scaled into [2^6, 2^7), the centres
+// into [2^4, 2^5): a coefficient times x stays below 2^14.
+constexpr int kTopSlices = 16;  // partial maxima of an expert's centres
+constexpr int kScaleT = 256;
+template <class T>
+__global__ __launch_bounds__(kScaleT) void scale_columns_kernel(const T* x, int64_t ldx, const float* scales, int group,
+                                                                int64_t width, int64_t t, const float* centers, int64_t per_expert,
+                                                                float* out, int32_t* exps, uint32_t* tops) {
+  __shared__ uint32_t part[kScaleT / 64];
+  uint32_t top = 0;
+  const int64_t row = blockIdx.x;
+  if (row < t) {
+    for (int64_t i = threadIdx.x * 8; i < width; i += kScaleT * 8) {
+      const int valid = width - i < 8 ? static_cast<int>(width - i) : 8;
+      float v[8];
+      load8(x + row * ldx + i, valid, v);
+      if (scales != nullptr) {
+        const float s = group ? scales[row * ((width + group - 1) / group) + i / group] : scales[row];
 #pragma unroll
-    for (int s = 0; s < kTT; ++s) {
-      if (s >= tl.rows) break;
-      const float xs = x[(tl.row0 + s) * a.m + i];
+        for (int j = 0; j < 8; ++j) v[j] *= s;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
+        top = b > top && j < valid ? b : top;
+      }
+      store8(out + row * width + i, valid, v);
+    }
+  } else {
+    const int64_t e = (row - t) / kTopSlices, slice = (row - t) % kTopSlices;
+    const float* ce = centers + e * per_expert;
+    for (int64_t i = (slice * kScaleT + threadIdx.x) * 4; i < per_expert; i += kTopSlices * kScaleT * 4) {
+      const float4_t v = *reinterpret_cast<const float4_t*>(ce + i);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        au[s][j] += pick(q, (cu >> (2 * j)) & 3) * xs;
-        av[s][j] += pick(q + 4, (cv >> (2 * j)) & 3) * xs;
+        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
+        top = b > top && b < kInfBits ? b : top;  // a row that is not finite gives NaN by itself
       }
     }
   }
 #pragma unroll
-  for (int s = 0; s < kTT; ++s) {
-    if (s >= tl.rows) break;
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_xor(top, d);
+    top = o > top ? o : top;
+  }
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = top;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      zu[(tl.row0 + s) * k + 4 * col + j] = au[s][j];
-      zv[(tl.row0 + s) * k + 4 * col + j] = av[s][j];
+  for (int w = 0; w < kScaleT / 64; ++w) top = part[w] > top ? part[w] : top;
+  if (row < t) exps[row] = top >= kInfBits ? 1024 : scale_exponent(top) - 7;  // 1024: the row is not finite
+  else tops[row - t] = top;
+}
+
+// The split of a transposed product: a workgroup of `waves` waves takes as many blocks of columns of one group, over
+// `rows` matrix rows (a multiple of 32), of which there are `splits` per matrix; their sums are joined afterwards.
+struct ColumnsPlan {
+  int j, steps, waves, per_group, splits;
+  int64_t rows, tiles;
+};
+
+template <int J, int STEPS, bool LO>
+__global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsPlan pl, const float* x, const int32_t* exps,
+                                                         const uint32_t* tops, float* out) {
+  constexpr int TT = tile_rows<J>(), JJ = J == 0 ? 1 : J, PARTS = LO && J != 0 ? 2 : 1, CP = 16 * JJ;
+  __shared__ __align__(16) _Float16 xs[2][4][PARTS][4][CP][8];  // [buffer][function][part][quarter][column of B][row]
+  __shared__ float xscale[TT];
+  const Tile tl = find_tile<TT>(a.offsets, a.experts, a.t, blockIdx.y);
+  if (tl.rows == 0) return;
+  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = tid / 64, r = lane % 16, q = lane / 16;
+  int id = blockIdx.x;
+  const int wblk = id % pl.per_group;
+  id /= pl.per_group;
+  const int g = id % a.groups;
+  id /= a.groups;
+  const int f = id % 2, split = id / 2;
+  const int unit = wblk * pl.waves + wave, block = unit * STEPS / 16, half = STEPS == 16 ? 0 : unit % 2;
+  const bool busy = block * 256 < n;
+  const int64_t i0 = split * pl.rows, i1 = i0 + pl.rows < a.m ? i0 + pl.rows : a.m;
+  uint32_t top = 0;
+#pragma unroll
+  for (int s = 0; s < kTopSlices; ++s) {
+    const uint32_t o = tops[tl.expert * kTopSlices + s];
+    top = o > top ? o : top;
+  }
+  const int ec = scale_exponent(top) - 9;
+  const float cscale = power_of_two(ec);
+  for (int c = tid; c < TT; c += blockDim.x) {
+    const int e = c < tl.rows ? exps[tl.row0 + c] : 0;
+    xscale[c] = e == 1024 ? __int_as_float(0x7fc00000) : power_of_two(e);
+  }
+  __syncthreads();
+
+  const uint8_t* codes = f ? a.codes_v : a.codes_u;
+  // the lane's dword of codes; at a group's end (n no multiple of 16, or past the last column) the last four bytes
+  // are read and moved down
+  int off = block * 64 + 4 * r, shift = 0;
+  if (off > nby - 4) {
+    shift = 8 * (off - (nby - 4));
+    shift = shift < 24 ? shift : 24;
+    off = nby - 4;
+  }
+  auto load_codes8 = [&](int64_t k0, uint32_t (&w)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int64_t i = k0 + 8 * q + e;
+      __builtin_memcpy(&w[e], codes + ((tl.expert * a.m + (i < a.m ? i : a.m - 1)) * a.groups + g) * nby + off, 4);
+    }
+  };
+  auto build = [&](int64_t k0, int buf) {
+    for (int it = tid; it < 16 * TT; it += blockDim.x) {
+      const int pair = it % 16, c = it / 16;
+      _Float16 h[2][4], l[2][4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int64_t i = k0 + 2 * pair + e;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (c < tl.rows && i < i1) {
+          const float4_t ce =
+              *reinterpret_cast<const float4_t*>(a.centers + ((tl.expert * a.m + i) * a.groups + g) * 8 + 4 * f) * cscale;
+          const float xv = x[(tl.row0 + c) * a.m + i] * xscale[c];
+          const float d = (ce[3] - ce[2]) - (ce[1] - ce[0]);
+          v[0] = xv * ce[0];
+          v[1] = xv * ((ce[1] - ce[0]) - d);
+          v[2] = xv * (0.5f * (ce[2] - ce[0]) - d);
+          v[3] = xv * d;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          h[e][k] = static_cast<_Float16>(v[k]);
+          l[e][k] = static_cast<_Float16>(v[k] - static_cast<float>(h[e][k]));
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        *reinterpret_cast<uint32_t*>(&xs[buf][k][0][pair / 4][c][2 * (pair % 4)]) = pair_bits(h[0][k], h[1][k]);
+        if constexpr (J == 0) *reinterpret_cast<uint32_t*>(&xs[buf][k][0][pair / 4][c + 8][2 * (pair % 4)]) = pair_bits(l[0][k], l[1][k]);
+        else if constexpr (LO) *reinterpret_cast<uint32_t*>(&xs[buf][k][PARTS - 1][pair / 4][c][2 * (pair % 4)]) = pair_bits(l[0][k], l[1][k]);
+      }
+    }
+  };
+
+  float4_t acc[JJ][STEPS], flat[JJ];
+#pragma unroll
+  for (int j = 0; j < JJ; ++j) {
+    flat[j] = float4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) acc[j][s] = float4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  uint32_t next[8];
+  if (busy) load_codes8(i0, next);
+  build(i0, 0);
+  __syncthreads();
+  int buf = 0;
+  for (int64_t k0 = i0; k0 < i1; k0 += 32, buf ^= 1) {
+    uint32_t w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = next[e] >> shift;
+    if (k0 + 32 < i1) {
+      if (busy) load_codes8(k0 + 32, next);
+      build(k0 + 32, buf ^ 1);
+    }
+    if (busy) {
+      half8 b[JJ][4][PARTS];
+#pragma unroll
+      for (int j = 0; j < JJ; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int pt = 0; pt < PARTS; ++pt) b[j][k][pt] = *reinterpret_cast<const half8*>(&xs[buf][k][pt][q][16 * j + r][0]);
+      uint4_t ones = {0x04000400u, 0x04000400u, 0x04000400u, 0x04000400u};
+#pragma unroll
+      for (int j = 0; j < JJ; ++j)
+#pragma unroll
+        for (int pt = 0; pt < PARTS; ++pt)
+          flat[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, ones), b[j][0][pt], flat[j], 0, 0, 0);
+      uint32_t p[2][4];  // low and high halves of the dwords, two rows side by side
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[0][e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], 0x05040100u);
+        p[1][e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], 0x07060302u);
+      }
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        uint4_t fn[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t v = STEPS == 16 ? p[s / 8][e] : (half ? p[1][e] : p[0][e]);
+          const int at = 2 * (s % 8);
+          const uint32_t c = at <= 10 ? v << (10 - at) : v >> (at - 10);
+          fn[0][e] = c & 0x04000400u;
+          fn[1][e] = c & 0x08000800u;
+          fn[2][e] = c & 0x0c000c00u;
+        }
+#pragma unroll
+        for (int j = 0; j < JJ; ++j)
+#pragma unroll
+          for (int pt = PARTS - 1; pt >= 0; --pt)
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+              acc[j][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, fn[k]), b[j][k + 1][pt], acc[j][s], 0, 0, 0);
+      }
+    }
+    __syncthreads();
+  }
+  if (!busy) return;
+  const int64_t k = static_cast<int64_t>(a.groups) * n;
+#pragma unroll
+  for (int j = 0; j < JJ; ++j) {
+    const int c = J == 0 ? r : 16 * j + r;
+    const bool mine = c < tl.rows;
+    const int64_t row = tl.row0 + (mine ? c : 0);
+    const int et = exps[row], unscale = 14 - ec - (et == 1024 ? 0 : et);
+    float* o = out + ((static_cast<int64_t>(split) * 2 + f) * a.t + row) * k + static_cast<int64_t>(g) * n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int col = block * 256 + (4 * q + i) * 16 + half * 8;
+#pragma unroll
+      for (int s0 = 0; s0 < STEPS; s0 += 4) {
+        float4_t v;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          float z = acc[j][s0 + s][i] + flat[j][i];
+          if constexpr (J == 0)  // the lo part's column
+            z += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(z), 0x128, 0xf, 0xf, true));
+          v[s] = ldexpf(z, unscale);
+        }
+        if (mine && (J != 0 || r < 8) && col + s0 < n) *reinterpret_cast<float4_t*>(o + col + s0) = v;
+      }
     }
   }
 }
@@ -419,18 +625,37 @@ __device__ __forceinline__ bool covered(const int64_t* offsets, int experts, int
   return offsets == nullptr || (row >= offsets[0] && row < offsets[experts]);
 }
 
-// Rows that no expert has, as zeros: P takes rows in pairs, and what lies in a row's neighbour may show in its last
-// bits.
-__global__ __launch_bounds__(256) void clear_spare_kernel(const int64_t* offsets, int experts, int64_t width, float* z) {
-  if (covered(offsets, experts, blockIdx.x)) return;
-  const int64_t i = static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x;
-  if (i < width) z[blockIdx.x * width + i] = 0.f;
+// zv = the sum of its parts; zeros for rows that no expert has (P takes rows in pairs, and what lies in a row's
+// neighbour may show in its last bits).
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int splits, const float* parts, int64_t k, float* zv) {
+  const int64_t row = blockIdx.x, i = (static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x) * 4;
+  if (i >= k) return;
+  float4_t v = {0.f, 0.f, 0.f, 0.f};
+  if (covered(a.offsets, a.experts, row))
+    for (int s = 0; s < splits; ++s)
+      v += *reinterpret_cast<const float4_t*>(parts + ((static_cast<int64_t>(s) * 2 + 1) * a.t + row) * k + i);
+  *reinterpret_cast<float4_t*>(zv + row * k + i) = v;
 }
 
-// z += pz (fp32 rows)
-__global__ __launch_bounds__(256) void add_kernel(float* z, const float* pz, int64_t count) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i < count) z[i] += pz[i];
+// y = zu + P zv, zu the sum of its parts: into y, or as fp32 rows into z (the rotation follows).
+__global__ __launch_bounds__(256) void finish_kernel(ProductArgs a, int splits, const float* parts, const float* pz, int64_t k,
+                                                     float* z) {
+  const int64_t row = blockIdx.x, i = (static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x) * 4;
+  if (i >= k) return;
+  float4_t v = {0.f, 0.f, 0.f, 0.f};
+  if (covered(a.offsets, a.experts, row)) {
+    for (int s = 0; s < splits; ++s)
+      v += *reinterpret_cast<const float4_t*>(parts + (static_cast<int64_t>(s) * 2 * a.t + row) * k + i);
+    v += *reinterpret_cast<const float4_t*>(pz + row * k + i);
+  } else if (z == nullptr) {
+    return;
+  }
+  if (z != nullptr) {
+    *reinterpret_cast<float4_t*>(z + row * k + i) = v;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) put(a.y, a.y_dtype, row * a.ldy + i + j, v[j]);
+  }
 }
 
 // y = z in y's type, covered rows only.
@@ -473,59 +698,126 @@ hipError_t rotate(const ProductArgs& a, bool inverse, float* z, hipStream_t s) {
 template <int J, int R>
 hipError_t launch_rows(const ProductArgs& a, const _Float16* frags, const int32_t* exps, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((a.m + 16 * R - 1) / (16 * R)),
-                  static_cast<unsigned>(most_tiles(a, tile_rows<J>())));
+                  static_cast<unsigned>(most_tiles(a.offsets != nullptr, a.t, a.experts, tile_rows<J>())));
   hipLaunchKernelGGL((rows_kernel<J, R>), grid, dim3(kRowsT), 0, s, a, frags, exps);
+  return hipGetLastError();
+}
+
+// Rows of x that a matrix (an expert's, on average) meets.
+int64_t rows_each(int64_t t, int experts) { return t / (experts < t ? experts : t > 0 ? t : 1); }
+
+ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts) {
+  ColumnsPlan p;
+  const int64_t each = rows_each(t, experts);
+  p.j = each <= 8 ? 0 : each <= 16 ? 1 : 2;
+  p.steps = 16;
+  const int units = (n + 255) / 256 * (16 / p.steps);
+  for (p.waves = 8; p.waves > 1; p.waves /= 2)  // at most an eighth of the waves idle
+    if (((units + p.waves - 1) / p.waves * p.waves - units) * 8 <= units) break;
+  p.per_group = (units + p.waves - 1) / p.waves;
+  p.tiles = most_tiles(experts > 1, t, experts, p.j == 0 ? 8 : 16 * p.j);
+  // enough workgroups to fill the chip twice over, of at least 64 rows each
+  const int64_t one = static_cast<int64_t>(p.per_group) * groups * 2 * (p.tiles > 0 ? p.tiles : 1);
+  const int64_t want = (512 * 8 / p.waves + one - 1) / one, most = (m + 63) / 64;
+  int64_t splits = want < most ? want : most;
+  p.rows = ((m + splits - 1) / splits + 31) / 32 * 32;
+  p.splits = static_cast<int>((m + p.rows - 1) / p.rows);
+  return p;
+}
+
+struct ColumnsWork {
+  int64_t x, exps, tops, zv, pz, parts, end;
+};
+ColumnsWork columns_work(const ColumnsPlan& p, int n, int64_t m, int groups, int64_t t, int experts) {
+  const int64_t k = static_cast<int64_t>(groups) * n;
+  ColumnsWork w;
+  w.x = 0;
+  w.exps = w.x + align256(t * m * 4);
+  w.tops = w.exps + align256(t * 4);
+  w.zv = w.tops + align256(static_cast<int64_t>(experts) * kTopSlices * 4);
+  w.pz = w.zv + align256(t * k * 4);
+  w.parts = w.pz + align256(t * k * 4);
+  w.end = w.parts + static_cast<int64_t>(p.splits) * 2 * t * k * 4;
+  return w;
+}
+
+template <int J, int STEPS, bool LO>
+hipError_t launch_columns(const ProductArgs& a, const ColumnsPlan& p, const float* x, const int32_t* exps,
+                          const uint32_t* tops, float* parts, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.per_group) * a.groups * 2 * p.splits),
+                  static_cast<unsigned>(p.tiles));
+  hipLaunchKernelGGL((columns_kernel<J, STEPS, LO>), grid, dim3(64 * p.waves), 0, s, a, p, x, exps, tops, parts);
+  return hipGetLastError();
+}
+
+hipError_t product_back(const ProductArgs& a, hipStream_t s) {
+  const int64_t k = static_cast<int64_t>(a.groups) * a.n;
+  const ColumnsPlan p = plan_columns(a.n, a.m, a.groups, a.t, a.experts);
+  const ColumnsWork at = columns_work(p, a.n, a.m, a.groups, a.t, a.experts);
+  float* x = reinterpret_cast<float*>(a.work + at.x);
+  int32_t* exps = reinterpret_cast<int32_t*>(a.work + at.exps);
+  uint32_t* tops = reinterpret_cast<uint32_t*>(a.work + at.tops);
+  float* zv = reinterpret_cast<float*>(a.work + at.zv);
+  float* pz = reinterpret_cast<float*>(a.work + at.pz);
+  float* parts = reinterpret_cast<float*>(a.work + at.parts);
+  const dim3 grid(static_cast<unsigned>(a.t + static_cast<int64_t>(a.experts) * kTopSlices));
+  const int64_t per_expert = a.m * a.groups * 8;
+  auto scale = [&](auto zero) {
+    using T = decltype(zero);
+    hipLaunchKernelGGL((scale_columns_kernel<T>), grid, dim3(kScaleT), 0, s, static_cast<const T*>(a.x), a.ldx, a.x_scales,
+                       a.x_group, a.m, a.t, a.centers, per_expert, x, exps, tops);
+    return hipGetLastError();
+  };
+  hipError_t e = a.x_dtype == KASHIN_E4M3 ? scale(e4m3_t()) : with_float_type(a.x_dtype, scale);
+  if (e != hipSuccess) return e;
+  e = p.j == 0   ? launch_columns<0, 16, true>(a, p, x, exps, tops, parts, s)
+      : p.j == 1 ? launch_columns<1, 16, true>(a, p, x, exps, tops, parts, s)
+                 : launch_columns<2, 16, true>(a, p, x, exps, tops, parts, s);
+  if (e != hipSuccess) return e;
+  const dim3 whole(static_cast<unsigned>(a.t), static_cast<unsigned>((k + 1023) / 1024));
+  hipLaunchKernelGGL(join_kernel, whole, dim3(256), 0, s, a, p.splits, parts, k, zv);
+  e = hipGetLastError();
+  if (e == hipSuccess) e = apply_p(a, zv, pz, s);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(finish_kernel, whole, dim3(256), 0, s, a, p.splits, parts, pz, k, a.rot ? zv : nullptr);
+  e = hipGetLastError();
+  if (e != hipSuccess || !a.rot) return e;
+  e = rotate(a, true, zv, s);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(narrow_kernel, dim3(static_cast<unsigned>(a.t), static_cast<unsigned>((k + 255) / 256)), dim3(256), 0, s,
+                     a, zv, k);
   return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t product_workspace_bytes(int n, int64_t m, int groups, int64_t t, int experts, bool back) {
-  (void)experts;
   const int64_t k = static_cast<int64_t>(groups) * n;
-  if (back) return align256(t * m * 4) + 3 * align256(t * k * 4);
+  if (t == 0) return 0;
+  if (back) return columns_work(plan_columns(n, m, groups, t, experts), n, m, groups, t, experts).end;
   return 2 * align256(t * k * 4) + align256(t * 4) + 4 * padded_chunks(n, groups) * kUnits * t * 16;
 }
 
 hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
-  const int64_t k = static_cast<int64_t>(a.groups) * a.n, wx = a.back ? a.m : k;
+  if (a.back) return product_back(a, s);
+  const int64_t k = static_cast<int64_t>(a.groups) * a.n;
   float* x = reinterpret_cast<float*>(a.work);
-  float* z[3];
-  for (int i = 0; i < 3; ++i) z[i] = reinterpret_cast<float*>(a.work + align256(a.t * wx * 4) + i * align256(a.t * k * 4));
-  const unsigned t = static_cast<unsigned>(a.t);
-  hipError_t e = widen(a, wx, x, s);
+  float* px = reinterpret_cast<float*>(a.work + align256(a.t * k * 4));
+  int32_t* exps = reinterpret_cast<int32_t*>(a.work + 2 * align256(a.t * k * 4));
+  _Float16* frags = reinterpret_cast<_Float16*>(a.work + 2 * align256(a.t * k * 4) + align256(a.t * 4));
+  hipError_t e = widen(a, k, x, s);
+  if (e == hipSuccess && a.rot) e = rotate(a, false, x, s);
+  if (e == hipSuccess) e = apply_p(a, x, px, s);
   if (e != hipSuccess) return e;
-  if (!a.back) {
-    if (a.rot) e = rotate(a, false, x, s);
-    if (e == hipSuccess) e = apply_p(a, x, z[0], s);
-    if (e != hipSuccess) return e;
-    int32_t* exps = reinterpret_cast<int32_t*>(a.work + 2 * align256(a.t * k * 4));
-    _Float16* frags = reinterpret_cast<_Float16*>(a.work + 2 * align256(a.t * k * 4) + align256(a.t * 4));
-    hipLaunchKernelGGL(split_rows_kernel, dim3(t), dim3(kSplitT), 0, s, x, z[0], a.n, a.groups, a.t, true, frags, exps);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int64_t each = a.offsets == nullptr ? a.t : a.t / (a.experts < a.t ? a.experts : a.t);
-    if (each <= 8) return launch_rows<0, 1>(a, frags, exps, s);
-    if (each <= 16) return launch_rows<1, 1>(a, frags, exps, s);
-    if (each <= 32) return launch_rows<2, 2>(a, frags, exps, s);
-    return launch_rows<4, 2>(a, frags, exps, s);
-  }
-  const dim3 whole(t, static_cast<unsigned>((k + 255) / 256));
-  if (a.offsets != nullptr) {
-    hipLaunchKernelGGL(clear_spare_kernel, whole, dim3(256), 0, s, a.offsets, a.experts, k, z[1]);
-    hipLaunchKernelGGL(clear_spare_kernel, whole, dim3(256), 0, s, a.offsets, a.experts, k, z[0]);
-  }
-  hipLaunchKernelGGL(columns_kernel, dim3(static_cast<unsigned>((k / 4 + 63) / 64), static_cast<unsigned>(most_tiles(a, kTT))),
-                     dim3(64), 0, s, a, x, z[0], z[1]);
+  hipLaunchKernelGGL(split_rows_kernel, dim3(static_cast<unsigned>(a.t)), dim3(kSplitT), 0, s, x, px, a.n, a.groups, a.t, true,
+                     frags, exps);
   e = hipGetLastError();
-  if (e == hipSuccess) e = apply_p(a, z[1], z[2], s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(add_kernel, dim3(static_cast<unsigned>((a.t * k + 255) / 256)), dim3(256), 0, s, z[0], z[2], a.t * k);
-  e = hipGetLastError();
-  if (e == hipSuccess && a.rot) e = rotate(a, true, z[0], s);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(narrow_kernel, whole, dim3(256), 0, s, a, z[0], k);
-  return hipGetLastError();
+  const int64_t each = rows_each(a.t, a.experts);
+  if (each <= 8) return launch_rows<0, 1>(a, frags, exps, s);
+  if (each <= 16) return launch_rows<1, 1>(a, frags, exps, s);
+  if (each <= 32) return launch_rows<2, 2>(a, frags, exps, s);
+  return launch_rows<4, 2>(a, frags, exps, s);
 }
 
 }  // namespace kashin
