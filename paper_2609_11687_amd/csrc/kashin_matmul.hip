@@ -91,6 +91,26 @@ __device__ __forceinline__ void put(void* y, int dtype, int64_t i, float v) {
   else static_cast<__bf16*>(y)[i] = static_cast<__bf16>(v);
 }
 
+template <class T>
+__device__ __forceinline__ void put4_as(T* y, int64_t valid, const float (&v)[4]) {
+  T q[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) q[j] = static_cast<T>(v[j]);
+  if (valid >= 4) {
+    __builtin_memcpy(y, q, sizeof(q));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < valid) y[j] = q[j];
+  }
+}
+// Four entries from i on, of which `valid` exist.
+__device__ __forceinline__ void put4(void* y, int dtype, int64_t i, int64_t valid, const float (&v)[4]) {
+  if (dtype == KASHIN_F32) put4_as(static_cast<float*>(y) + i, valid, v);
+  else if (dtype == KASHIN_F16) put4_as(static_cast<_Float16*>(y) + i, valid, v);
+  else put4_as(static_cast<__bf16*>(y) + i, valid, v);
+}
+
 // ------------------------------------------------------------------ operands of the matrix instructions
 // Products run on fp16 matrix instructions with fp32 sums.  fp32 operands are two fp16 parts, hi + lo, which hold 22
 // bits: x y = hi hi + hi lo + lo hi to 2^-21.  Both operands are scaled by powers of two first, a row of x with P x and a
@@ -251,7 +271,7 @@ constexpr int kRowsT = 512;
 template <int J>
 constexpr int tile_rows() { return J == 0 ? 8 : 16 * J; }
 
-template <int J, int R>
+template <int J, int R, bool LO>
 __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _Float16* frags, const int32_t* exps) {
   constexpr int TT = tile_rows<J>(), JJ = J == 0 ? 1 : J, NW = kRowsT / 64, RP = 16 * R + 4;
   __shared__ float sums[NW][16 * JJ][RP];
@@ -344,16 +364,16 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
       for (int s = 0; s < kUnits; ++s) {
         half8 hi[R], lo[R];
 #pragma unroll
-        for (int i = 0; i < R; ++i) decode8<true>(now[i][s / 2], s % 2, tb[i], hi[i], lo[i]);
+        for (int i = 0; i < R; ++i) decode8<LO>(now[i][s / 2], s % 2, tb[i], hi[i], lo[i]);
 #pragma unroll
         for (int j = 0; j < JJ; ++j) {
           const half8 xh = *reinterpret_cast<const half8*>(col[j] + (unit0 + s) * a.t * 8);
           half8 xl = {};
-          if constexpr (J != 0) xl = *reinterpret_cast<const half8*>(col[j] + (unit0 + s + 2 * units) * a.t * 8);
+          if constexpr (J != 0 && LO) xl = *reinterpret_cast<const half8*>(col[j] + (unit0 + s + 2 * units) * a.t * 8);
 #pragma unroll
           for (int i = 0; i < R; ++i) {
-            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[i], xh, acc[j][i], 0, 0, 0);
-            if constexpr (J != 0) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[i], xl, acc[j][i], 0, 0, 0);
+            if constexpr (LO) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[i], xh, acc[j][i], 0, 0, 0);
+            if constexpr (J != 0 && LO) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[i], xl, acc[j][i], 0, 0, 0);
             acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[i], xh, acc[j][i], 0, 0, 0);
           }
         }
@@ -374,6 +394,154 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
     const uint32_t top = tops[i];
     const int e = top >= kInfBits ? 0 : scale_exponent(top);
     put(a.y, a.y_dtype, (tl.row0 + c) * a.ldy + row0 + i, ldexpf(v, -(e + exps[tl.row0 + c])));
+  }
+}
+
+// y = x W^T for many rows of x: a workgroup computes 256 matrix rows by 128 rows of x, wave (rw, cw) 64 by 64 of them in
+// 32 x 32 tiles.  The rows of x pass through LDS (128 entries of K of one factor at a time, two buffers, filled by loads
+// that go to LDS directly); a wave decodes its 64 matrix rows' codes in registers, each code once for 64 rows of x.
+using float16_t = float __attribute__((ext_vector_type(16)));
+constexpr int kTileM = 256, kTileT = 128;
+
+// Loads to LDS of this wave have arrived (a barrier alone does not wait for them).
+__device__ __forceinline__ void wait_lds_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void load_to_lds(const void* from, void* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+template <bool LO>
+__global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const _Float16* frags, const int32_t* exps) {
+  constexpr int PARTS = LO ? 2 : 1, SU = 2 * kUnits;  // units of a slab: two chunks
+  __shared__ __align__(16) _Float16 xs[2][PARTS][SU][kTileT][8];
+  __shared__ uint32_t tops[kTileM];
+  const Tile tl = find_tile<kTileT>(a.offsets, a.experts, a.t, blockIdx.y);
+  if (tl.rows == 0) return;
+  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int r = lane % 32, q = lane / 32, rw = wave / 2, cw = wave % 2, cpg = chunks_per_group(n);
+  const int chunks = a.groups * cpg;
+  const int64_t units = padded_chunks(n, a.groups) * kUnits;
+  const int slabs = (chunks + 1) / 2, items = 2 * slabs;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTileM;
+  int64_t first[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t row = row0 + 64 * rw + 32 * i + r;
+    first[i] = (tl.expert * a.m + (row < a.m ? row : a.m - 1)) * a.groups;
+  }
+  auto load_item = [&](int it, uint4_t (&c)[2]) {
+    const int f = it >= slabs, chunk = (it - f * slabs) * 2 + q;
+    const uint8_t* base = f ? a.codes_v : a.codes_u;
+    const int at = chunk < chunks ? chunk : chunks - 1;
+    const int g = a.groups == 1 ? 0 : at / cpg, off = (at - g * cpg) * 16;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) c[i] = load_codes(base + (first[i] + g) * nby, nby, off);
+  };
+  auto fill = [&](int it, int buf) {
+    const int f = it >= slabs;
+    const int64_t u0 = f * units + static_cast<int64_t>(it - f * slabs) * SU;
+#pragma unroll
+    for (int pt = 0; pt < PARTS; ++pt)
+#pragma unroll
+      for (int k = 0; k < SU / 4; ++k) {
+        const int u = 4 * k + wave / 2, c = (wave % 2) * 64 + lane;
+        const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
+        load_to_lds(frags + ((u0 + u + pt * 2 * units) * a.t + row) * 8, &xs[buf][pt][u][(wave % 2) * 64][0]);
+      }
+  };
+  uint4_t next[2];
+  load_item(0, next);
+  fill(0, 0);
+  if (tid < kTileM) tops[tid] = 0;
+  __syncthreads();
+  {
+    uint32_t top = 0;
+    const int mine = tid % kTileM;
+    const int64_t row = row0 + mine;
+    const float* ce = a.centers + (tl.expert * a.m + (row < a.m ? row : a.m - 1)) * a.groups * 8;
+    for (int64_t j = tid / kTileM; j < a.groups * 2; j += 512 / kTileM) {
+      const float4_t v = *reinterpret_cast<const float4_t*>(ce + 4 * j);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t b = __float_as_uint(v[k]) & 0x7fffffffu;
+        top = b > top ? b : top;
+      }
+    }
+    if (top) atomicMax(&tops[mine], top);  // a maximum: the same in any order
+  }
+  wait_lds_loads();
+  __syncthreads();
+  float scale[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t top = tops[64 * rw + 32 * i + r];
+    scale[i] = top >= kInfBits ? __int_as_float(0x7fc00000) : power_of_two(scale_exponent(top));
+  }
+  float16_t acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
+  Table tb[2];
+  int held = -1;
+  for (int it = 0; it < items; ++it) {
+    const int buf = it & 1, f = it >= slabs, chunk = (it - f * slabs) * 2 + q;
+    const int g = a.groups == 1 ? 0 : (chunk < chunks ? chunk : chunks - 1) / cpg;
+    uint4_t now[2] = {next[0], next[1]};
+    if (it + 1 < items) {
+      fill(it + 1, buf ^ 1);
+      load_item(it + 1, next);
+    }
+    if (f * a.groups + g != held) {
+      held = f * a.groups + g;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        tb[i] = make_table(*reinterpret_cast<const float4_t*>(a.centers + (first[i] + g) * 8 + 4 * f), scale[i]);
+    }
+#pragma unroll
+    for (int s = 0; s < kUnits; ++s) {
+      half8 hi[2], lo[2], xh[2], xl[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        xh[j] = *reinterpret_cast<const half8*>(&xs[buf][0][q * kUnits + s][64 * cw + 32 * j + r][0]);
+        if constexpr (LO) xl[j] = *reinterpret_cast<const half8*>(&xs[buf][1][q * kUnits + s][64 * cw + 32 * j + r][0]);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) decode8<LO>(now[i][s / 2], s % 2, tb[i], hi[i], lo[i]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if constexpr (LO) {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo[i], xh[j], acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi[i], xl[j], acc[i][j], 0, 0, 0);
+          }
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi[i], xh[j], acc[i][j], 0, 0, 0);
+        }
+    }
+    wait_lds_loads();
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int c = 64 * cw + 32 * j + r;
+    if (c >= tl.rows) continue;
+    const int ex = exps[tl.row0 + c];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const int in_tile = 64 * rw + 32 * i + 8 * b + 4 * q;
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t top = tops[in_tile + k];
+          v[k] = ldexpf(acc[i][j][4 * b + k], -((top >= kInfBits ? 0 : scale_exponent(top)) + ex));
+        }
+        put4(a.y, a.y_dtype, (tl.row0 + c) * a.ldy + row0 + in_tile, a.m - row0 - in_tile, v);
+      }
   }
 }
 
@@ -695,11 +863,11 @@ hipError_t rotate(const ProductArgs& a, bool inverse, float* z, hipStream_t s) {
   return launch_rotate(a.n, a.rot_seed, inverse, z, KASHIN_F32, a.n, z, a.n, a.t * a.groups, s);
 }
 
-template <int J, int R>
+template <int J, int R, bool LO>
 hipError_t launch_rows(const ProductArgs& a, const _Float16* frags, const int32_t* exps, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((a.m + 16 * R - 1) / (16 * R)),
                   static_cast<unsigned>(most_tiles(a.offsets != nullptr, a.t, a.experts, tile_rows<J>())));
-  hipLaunchKernelGGL((rows_kernel<J, R>), grid, dim3(kRowsT), 0, s, a, frags, exps);
+  hipLaunchKernelGGL((rows_kernel<J, R, LO>), grid, dim3(kRowsT), 0, s, a, frags, exps);
   return hipGetLastError();
 }
 
@@ -805,19 +973,29 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
   float* px = reinterpret_cast<float*>(a.work + align256(a.t * k * 4));
   int32_t* exps = reinterpret_cast<int32_t*>(a.work + 2 * align256(a.t * k * 4));
   _Float16* frags = reinterpret_cast<_Float16*>(a.work + 2 * align256(a.t * k * 4) + align256(a.t * 4));
+  // bf16 results are rounded by 2^-9 each; operands rounded to fp16 (2^-12) add nothing to speak of
+  const int64_t each = rows_each(a.t, a.experts);
+  const bool lo = each <= 16 || a.y_dtype != KASHIN_BF16;
   hipError_t e = widen(a, k, x, s);
   if (e == hipSuccess && a.rot) e = rotate(a, false, x, s);
   if (e == hipSuccess) e = apply_p(a, x, px, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(split_rows_kernel, dim3(static_cast<unsigned>(a.t)), dim3(kSplitT), 0, s, x, px, a.n, a.groups, a.t, true,
+  hipLaunchKernelGGL(split_rows_kernel, dim3(static_cast<unsigned>(a.t)), dim3(kSplitT), 0, s, x, px, a.n, a.groups, a.t, lo,
                      frags, exps);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t each = rows_each(a.t, a.experts);
-  if (each <= 8) return launch_rows<0, 1>(a, frags, exps, s);
-  if (each <= 16) return launch_rows<1, 1>(a, frags, exps, s);
-  if (each <= 32) return launch_rows<2, 2>(a, frags, exps, s);
-  return launch_rows<4, 2>(a, frags, exps, s);
+  if (each <= 8) return launch_rows<0, 1, true>(a, frags, exps, s);
+  if (each <= 16) return launch_rows<1, 1, true>(a, frags, exps, s);
+  // enough tiles of 256 x 128 to fill the chip
+  if (each >= 96 && ((a.m + kTileM - 1) / kTileM) * (a.t / kTileT) >= 128) {
+    const dim3 grid(static_cast<unsigned>((a.m + kTileM - 1) / kTileM),
+                    static_cast<unsigned>(most_tiles(a.offsets != nullptr, a.t, a.experts, kTileT)));
+    if (lo) hipLaunchKernelGGL((rows_tile_kernel<true>), grid, dim3(512), 0, s, a, frags, exps);
+    else hipLaunchKernelGGL((rows_tile_kernel<false>), grid, dim3(512), 0, s, a, frags, exps);
+    return hipGetLastError();
+  }
+  if (lo) return each <= 32 ? launch_rows<2, 2, true>(a, frags, exps, s) : launch_rows<4, 2, true>(a, frags, exps, s);
+  return each <= 32 ? launch_rows<2, 2, false>(a, frags, exps, s) : launch_rows<4, 2, false>(a, frags, exps, s);
 }
 
 }  // namespace kashin

@@ -265,6 +265,22 @@ def test_products_of_groups_and_rotations(n, groups, m, rot, back):
 
 
 @pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("n,groups,m,t", [(256, 2, 4100, 1050), (64, 1, 33000, 200), (96, 3, 8200, 511), (512, 1, 2100, 2049)])
+def test_products_of_many_rows(n, groups, m, t, back):
+    print(f"product n={n} groups={groups} m={m} t={t} back={back}", flush=True)
+    case = Case(n, m, groups)
+    for dtype, out in (("bf16", "bf16"), ("f32", "f32")):
+        x, y = _product(case, t, dtype, out, back)
+        _check(case, y, x, out, back)
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_experts_of_many_rows(back):
+    for out in ("f32", "f16"):
+        _experts(Case(256, 4100, 1, experts=5), [150, 0, 900, 128, 33], 1215, "bf16", out, back, 1)
+
+
+@pytest.mark.parametrize("back", [False, True])
 @pytest.mark.parametrize("dtype,out", [("f32", "f16"), ("f16", "f32"), ("bf16", "bf16"), ("e4m3", "bf16")])
 def test_products_of_strided_and_unaligned_rows(dtype, out, back):
     case = Case(256, 61, 3)
