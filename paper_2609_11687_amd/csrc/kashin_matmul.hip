@@ -17,6 +17,14 @@ __device__ __forceinline__ void expert_rows(const int64_t* offsets, int e, int64
   hi = hi < lo ? lo : hi > t ? t : hi;
 }
 
+// A value that is the same in all lanes, as the compiler can use it for scalar addresses and branches.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(v));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<int>(v >> 32));
+  return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
+}
+
 // Tile number `tile` of at most TT rows that belong to one expert, tiles counted over the experts in turn; rows 0
 // past the last tile.  Every lane of the wave calls it.
 struct Tile {
@@ -50,12 +58,12 @@ __device__ Tile find_tile(const int64_t* offsets, int experts, int64_t t, int ti
       const int f = __ffsll(static_cast<unsigned long long>(past)) - 1;
       const int first = before + __shfl(upto - tiles, f);
       const int64_t l = __shfl(static_cast<long long>(lo), f), h = __shfl(static_cast<long long>(hi), f);
-      r.expert = e0 + f;
-      r.row0 = l + static_cast<int64_t>(tile - first) * TT;
-      r.rows = static_cast<int>(h - r.row0 < TT ? h - r.row0 : TT);
+      r.expert = uniform(e0 + f);
+      r.row0 = uniform(l + static_cast<int64_t>(tile - first) * TT);
+      r.rows = uniform(static_cast<int>(h - r.row0 < TT ? h - r.row0 : TT));
       return r;
     }
-    before += __shfl(upto, 63);
+    before += uniform(__shfl(upto, 63));
   }
   return r;
 }
@@ -63,6 +71,18 @@ __device__ Tile find_tile(const int64_t* offsets, int experts, int64_t t, int ti
 int64_t most_tiles(bool grouped, int64_t t, int experts, int64_t tt) {
   if (!grouped) return (t + tt - 1) / tt;
   return t / tt + (experts < t ? experts : t);
+}
+
+// Rows of x as a kernel reads them: the caller's (fp32, fp16, bf16) or fp32 ones in the workspace.
+struct XRows {
+  const void* p;
+  int64_t ld;
+  int dtype;
+};
+__device__ __forceinline__ void load_row8(const XRows& x, int64_t at, int valid, float (&v)[8]) {
+  if (x.dtype == KASHIN_F32) load8(static_cast<const float*>(x.p) + at, valid, v);
+  else if (x.dtype == KASHIN_F16) load8(static_cast<const _Float16*>(x.p) + at, valid, v);
+  else load8(static_cast<const __bf16*>(x.p) + at, valid, v);
 }
 
 // x as contiguous fp32 rows.
@@ -121,6 +141,7 @@ using uint4_t = uint32_t __attribute__((ext_vector_type(4)));
 
 constexpr int kChunk = 64;  // codes a lane decodes from one 16-byte load
 constexpr int kUnits = 8;   // units of 8 codes in a chunk: one operand register block of a matrix instruction each
+constexpr int kRowsT = 512;
 constexpr int kSlab = 4;    // chunks that the four quarters of a wave work on side by side
 
 __host__ __device__ inline int chunks_per_group(int n) { return (n + kChunk - 1) / kChunk; }
@@ -208,57 +229,83 @@ __device__ __forceinline__ uint4_t load_codes(const uint8_t* group, int nby, int
 }
 
 // ------------------------------------------------------------------ x W^T: x and P x as operands
-// frags[part][factor][unit][row][8]: hi (part 0) and lo parts of scaled x (factor 0) and P x, eight entries of a row
-// in the order of a unit's codes; rows innermost, so that the lanes of a matrix instruction's operand read consecutive 16
-// bytes.  exps[row]: the exponent of the scale.  One workgroup a row.
+// frags[factor][unit][part][row][8]: hi (part 0) and, where there are `parts` = 2, lo parts of scaled x (factor 0) and
+// P x, eight entries of a row in the order of a unit's codes; rows innermost, so that the lanes of a matrix instruction's
+// operand read consecutive 16 bytes.  exps[row]: the exponent of the scale.  One workgroup a row.
+// A workgroup takes ROWS rows (8: the lanes of eight rows write 128 consecutive bytes; 1 where there are few
+// rows, to spread them over the chip), a thread 16 entries of a row at a time: two units.
 constexpr int kSplitT = 512;
-__global__ __launch_bounds__(kSplitT) void split_rows_kernel(const float* x, const float* px, int n, int groups, int64_t t,
-                                                             bool lo, _Float16* frags, int32_t* exps) {
-  __shared__ uint32_t part[kSplitT / 64];
-  const int64_t row = blockIdx.x, k = static_cast<int64_t>(groups) * n;
-  const float* src[2] = {x + row * k, px + row * k};
-  uint32_t top = 0;
-  for (int f = 0; f < 2; ++f)
-    for (int64_t i = threadIdx.x * 4; i < k; i += kSplitT * 4) {  // n is a multiple of 4
-      const float4_t v = *reinterpret_cast<const float4_t*>(src[f] + i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
-        top = b > top ? b : top;
-      }
+template <int ROWS>
+__global__ __launch_bounds__(kSplitT) void split_rows_kernel(XRows x, const float* px, int n, int groups, int64_t t, int parts,
+                                                             _Float16* frags, int32_t* exps) {
+  __shared__ uint32_t tops[ROWS];
+  const int tid = threadIdx.x, mine = tid % ROWS;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + mine, k = static_cast<int64_t>(groups) * n;
+  const bool real = row < t;
+  const XRows src[2] = {x, {px, k, KASHIN_F32}};
+  const int per_group = chunks_per_group(n) * (kChunk / 16);
+  const int64_t blocks = padded_chunks(n, groups) * (kChunk / 16), used = static_cast<int64_t>(groups) * per_group;
+  auto load16 = [&](int f, int64_t b, float (&v)[16]) {  // block b of a factor, zeros past its group
+    int left = 0;
+    int64_t at = 0;
+    if (real && b < used) {
+      const int64_t g = b / per_group;
+      const int in_group = static_cast<int>(b - g * per_group) * 16;
+      at = row * src[f].ld + g * n + in_group;
+      left = n - in_group;
     }
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
+    for (int h = 0; h < 2; ++h) {
+      float u[8];
+      load_row8(src[f], at + 8 * h, left - 8 * h, u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[8 * h + j] = u[j];
+    }
+  };
+  if (tid < ROWS) tops[tid] = 0;
+  __syncthreads();
+  uint32_t top = 0;
+  for (int64_t b = tid / ROWS; b < 2 * used; b += kSplitT / ROWS) {
+    float v[16];
+    if (b < used) load16(0, b, v);
+    else load16(1, b - used, v);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const uint32_t o = __float_as_uint(v[j]) & 0x7fffffffu;
+      top = o > top ? o : top;
+    }
+  }
+#pragma unroll
+  for (int d = ROWS; d < 64; d <<= 1) {
     const uint32_t o = __shfl_xor(top, d);
     top = o > top ? o : top;
   }
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = top;
+  if (tid % 64 < ROWS) atomicMax(&tops[mine], top);  // a maximum: the same in any order
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSplitT / 64; ++w) top = part[w] > top ? part[w] : top;
+  top = tops[mine];
   const bool bad = top >= kInfBits;
   const int e = bad ? 0 : scale_exponent(top);
   const float scale = bad ? __int_as_float(0x7fc00000) : power_of_two(e);
-  if (threadIdx.x == 0) exps[row] = e;
-  const int cpg = chunks_per_group(n);
-  const int64_t units = padded_chunks(n, groups) * kUnits, real = static_cast<int64_t>(groups) * cpg * kUnits;
-  for (int64_t u = threadIdx.x; u < 2 * units; u += kSplitT) {
-    const int f = u >= units;
-    const int64_t un = u - f * units;
-    half8 h = {}, l = {};
-    if (un < real) {
-      const int g = static_cast<int>(un / (cpg * kUnits)), in_group = static_cast<int>(un % (cpg * kUnits));
-      const int base = in_group / kUnits * kChunk, unit = in_group % kUnits;
+  if (tid < ROWS && real) exps[row] = e;
+  if (!real) return;
+  for (int64_t b = tid / ROWS; b < 2 * blocks; b += kSplitT / ROWS) {
+    float v[16];
+    if (b < blocks) load16(0, b, v);
+    else load16(1, b - blocks, v);
+    half8 h[2], l[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int at = base + unit_entry(unit, j);
-        const float v = at < n ? src[f][static_cast<int64_t>(g) * n + at] * scale : 0.f;
-        h[j] = static_cast<_Float16>(v);
-        l[j] = static_cast<_Float16>(v - static_cast<float>(h[j]));
+        const float w = v[unit_entry(u, j)] * scale;
+        h[u][j] = static_cast<_Float16>(w);
+        l[u][j] = static_cast<_Float16>(w - static_cast<float>(h[u][j]));
       }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      *reinterpret_cast<half8*>(frags + ((2 * b + u) * parts * t + row) * 8) = h[u];
+      if (parts == 2) *reinterpret_cast<half8*>(frags + ((2 * b + u) * 2 * t + t + row) * 8) = l[u];
     }
-    *reinterpret_cast<half8*>(frags + (u * t + row) * 8) = h;
-    if (lo) *reinterpret_cast<half8*>(frags + ((u + 2 * units) * t + row) * 8) = l;
   }
 }
 
@@ -266,55 +313,93 @@ __global__ __launch_bounds__(kSplitT) void split_rows_kernel(const float* x, con
 // eighth of the codes each and their sums joined through LDS in a fixed order.  Operand A: lane (r, q) decodes chunk
 // 4 s + q of matrix row r, operand B: the same chunk's entries of x's rows.  J tiles of 16 rows of x, or J = 0: 8
 // rows, whose hi parts are B's columns 0 .. 7 and lo parts columns 8 .. 15, so that two instructions give all four products
-// (against three for 16 rows).
-constexpr int kRowsT = 512;
+// (against three for 16 rows).  LO: both operands in two parts; without it (J > 0) in one.  ALIGNED: n is a multiple of 256, so
+// that a slab lies in one group and no chunk is short: addresses and branches are scalar then.
 template <int J>
 constexpr int tile_rows() { return J == 0 ? 8 : 16 * J; }
 
-template <int J, int R, bool LO>
+template <int J, int R, bool LO, bool ALIGNED>
 __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _Float16* frags, const int32_t* exps) {
   constexpr int TT = tile_rows<J>(), JJ = J == 0 ? 1 : J, NW = kRowsT / 64, RP = 16 * R + 4;
+  constexpr int PARTS = J != 0 && LO ? 2 : 1;    // operands B for a unit and tile
+  constexpr int STORED = LO ? 2 : 1;             // parts in frags
+  constexpr int PF = JJ * PARTS <= 2 ? 4 : JJ * PARTS <= 4 ? 2 : 1;  // units whose x is loaded ahead: 16 .. 32 registers
   __shared__ float sums[NW][16 * JJ][RP];
   __shared__ uint32_t tops[16 * R];
   const Tile tl = find_tile<TT>(a.offsets, a.experts, a.t, blockIdx.y);
   if (tl.rows == 0) return;
-  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int r = lane % 16, q = lane / 16, cpg = chunks_per_group(n);
-  const int chunks = a.groups * cpg;
-  const int slabs = static_cast<int>(padded_chunks(n, a.groups) / kSlab);
-  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * (16 * R);
-  // matrix rows past the last repeat it
-  int64_t first[R];  // this lane's rows, as the first of their groups' rows of codes
+  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
+  const int r = lane % 16, q = lane / 16, cpg = chunks_per_group(n), groups = a.groups;
+  const int chunks = groups * cpg;
+  const int slabs = static_cast<int>(padded_chunks(n, groups) / kSlab), per_group = slabs / groups;  // per_group: ALIGNED
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * (16 * R), matrix0 = (tl.expert * a.m + row0) * groups;
+  // this lane's matrix rows (past the last repeat it), as offsets from the workgroup's first
+  uint32_t crow[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    const int64_t row = row0 + 16 * i + r;
-    first[i] = (tl.expert * a.m + (row < a.m ? row : a.m - 1)) * a.groups;
+    const int64_t left = a.m - 1 - row0;
+    crow[i] = static_cast<uint32_t>((16 * i + r < left ? 16 * i + r : left) * groups);
   }
+  const uint8_t* cu = a.codes_u + matrix0 * nby;
+  const uint8_t* cv = a.codes_v + matrix0 * nby;
+  const float* ce = a.centers + matrix0 * 8;
   // this wave's items: item = factor * slabs + slab
   const int items = 2 * slabs, i0 = items * wave / NW, i1 = items * (wave + 1) / NW;
   constexpr int AHEAD = 3;
   uint4_t codes[AHEAD][R];
   auto load_item = [&](int it, uint4_t (&c)[R]) {
-    const int f = it >= slabs, chunk = (it - f * slabs) * kSlab + q;
-    const uint8_t* base = f ? a.codes_v : a.codes_u;
-    const int at = chunk < chunks ? chunk : chunks - 1;
-    const int g = a.groups == 1 ? 0 : at / cpg, off = (at - g * cpg) * 16;
+    const int f = it >= slabs, slab = it - f * slabs;
+    const uint8_t* base = f ? cv : cu;
+    if constexpr (ALIGNED) {
+      base += slab * 64;
 #pragma unroll
-    for (int i = 0; i < R; ++i) c[i] = load_codes(base + (first[i] + g) * nby, nby, off);
+      for (int i = 0; i < R; ++i)
+        __builtin_memcpy(&c[i], base + static_cast<uint32_t>(crow[i] * static_cast<uint32_t>(nby) + 16 * q), 16);
+    } else {
+      const int chunk = slab * kSlab + q, at = chunk < chunks ? chunk : chunks - 1, g = at / cpg;
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        c[i] = load_codes(base + static_cast<uint32_t>((crow[i] + g) * static_cast<uint32_t>(nby)), nby, (at - g * cpg) * 16);
+    }
   };
 #pragma unroll
   for (int d = 0; d < AHEAD; ++d)
     if (i0 + d < i1) load_item(i0 + d, codes[d]);
+  // B: column c of tile j is row 16 j + c of the tile (J = 0: row c % 8, hi or lo part); columns past the last repeat it
+  const uint32_t t = static_cast<uint32_t>(a.t);
+  uint32_t col[JJ];
+#pragma unroll
+  for (int j = 0; j < JJ; ++j) {
+    int c = J == 0 ? r % 8 : 16 * j + r;
+    c = c < tl.rows ? c : tl.rows - 1;
+    col[j] = (q * kUnits * STORED * t + (J == 0 && r >= 8 ? t : 0) + c) * 16;
+  }
+  const char* x0 = reinterpret_cast<const char*>(frags + tl.row0 * 8);
+  half8 ahead[PF][JJ][PARTS];
+  auto load_x = [&](int it, int s0) {
+    // a buffer of its own for each item: the lanes' 32-bit offsets stay in registers, the units' are scalars
+    const auto units = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(x0) + static_cast<int64_t>(it) * (kSlab * kUnits) * STORED * t * 16, 0, -1, 0x00027000);
+#pragma unroll
+    for (int s = 0; s < PF; ++s)
+#pragma unroll
+      for (int j = 0; j < JJ; ++j)
+#pragma unroll
+        for (int pt = 0; pt < PARTS; ++pt)
+          ahead[s][j][pt] = __builtin_bit_cast(
+              half8, __builtin_amdgcn_raw_buffer_load_b128(units, col[j], ((s0 + s) * STORED + pt) * t * 16, 0));
+  };
+  if (i0 < i1) load_x(i0, 0);
   // the scale of every matrix row: its largest centre over all groups
   if (tid < 16 * R) tops[tid] = 0;
   __syncthreads();
   {
     uint32_t top = 0;
     const int mine = tid % (16 * R);
-    const int64_t row = row0 + mine;
-    const float* ce = a.centers + (tl.expert * a.m + (row < a.m ? row : a.m - 1)) * a.groups * 8;
-    for (int64_t j = tid / (16 * R); j < a.groups * 8; j += kRowsT / (16 * R)) {
-      const uint32_t b = __float_as_uint(ce[j]) & 0x7fffffffu;
+    const int64_t left = a.m - 1 - row0;
+    const float* mc = ce + static_cast<uint32_t>((mine < left ? mine : left) * groups) * 8u;
+    for (int j = tid / (16 * R); j < groups * 8; j += kRowsT / (16 * R)) {
+      const uint32_t b = __float_as_uint(mc[j]) & 0x7fffffffu;
       top = b > top ? b : top;
     }
     if (top) atomicMax(&tops[mine], top);  // a maximum: the same in any order
@@ -325,15 +410,6 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
   for (int i = 0; i < R; ++i) {
     const uint32_t top = tops[16 * i + r];
     scale[i] = top >= kInfBits ? __int_as_float(0x7fc00000) : power_of_two(scale_exponent(top));
-  }
-  // B: column c of tile j is row 16 j + c of the tile (J = 0: row c % 8, hi or lo part); columns past the last repeat it
-  const int64_t units = static_cast<int64_t>(slabs) * kSlab * kUnits;
-  const _Float16* col[JJ];
-#pragma unroll
-  for (int j = 0; j < JJ; ++j) {
-    int c = J == 0 ? r % 8 : 16 * j + r;
-    c = c < tl.rows ? c : tl.rows - 1;
-    col[j] = frags + (tl.row0 + c) * 8 + (J == 0 && r >= 8 ? 2 * units * a.t * 8 : 0);
   }
   float4_t acc[JJ][R];
 #pragma unroll
@@ -347,36 +423,52 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
     for (int d = 0; d < AHEAD; ++d) {
       const int it = b0 + d;
       if (it >= i1) break;
-      const int f = it >= slabs, chunk = (it - f * slabs) * kSlab + q;
-      const int g = a.groups == 1 ? 0 : (chunk < chunks ? chunk : chunks - 1) / cpg;
-      const int64_t unit0 = f * units + static_cast<int64_t>(chunk) * kUnits;
-      if (f * a.groups + g != held) {
-        held = f * a.groups + g;
+      const int f = it >= slabs, slab = it - f * slabs;
+      int g;
+      if constexpr (ALIGNED) {
+        g = groups == 1 ? 0 : slab / per_group;
+      } else {
+        const int chunk = slab * kSlab + q;
+        g = (chunk < chunks ? chunk : chunks - 1) / cpg;
+      }
+      if (f * groups + g != held) {
+        held = f * groups + g;
 #pragma unroll
         for (int i = 0; i < R; ++i)
-          tb[i] = make_table(*reinterpret_cast<const float4_t*>(a.centers + (first[i] + g) * 8 + 4 * f), scale[i]);
+          tb[i] = make_table(*reinterpret_cast<const float4_t*>(ce + 8 * g + 4 * f + static_cast<uint32_t>(crow[i] * 8)), scale[i]);
       }
       uint4_t now[R];
 #pragma unroll
       for (int i = 0; i < R; ++i) now[i] = codes[d][i];
       if (it + AHEAD < i1) load_item(it + AHEAD, codes[d]);
 #pragma unroll
-      for (int s = 0; s < kUnits; ++s) {
-        half8 hi[R], lo[R];
+      for (int s0 = 0; s0 < kUnits; s0 += PF) {
+        half8 x[PF][JJ][PARTS];
 #pragma unroll
-        for (int i = 0; i < R; ++i) decode8<LO>(now[i][s / 2], s % 2, tb[i], hi[i], lo[i]);
+        for (int s = 0; s < PF; ++s)
 #pragma unroll
-        for (int j = 0; j < JJ; ++j) {
-          const half8 xh = *reinterpret_cast<const half8*>(col[j] + (unit0 + s) * a.t * 8);
-          half8 xl = {};
-          if constexpr (J != 0 && LO) xl = *reinterpret_cast<const half8*>(col[j] + (unit0 + s + 2 * units) * a.t * 8);
+          for (int j = 0; j < JJ; ++j)
 #pragma unroll
-          for (int i = 0; i < R; ++i) {
-            if constexpr (LO) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[i], xh, acc[j][i], 0, 0, 0);
-            if constexpr (J != 0 && LO) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[i], xl, acc[j][i], 0, 0, 0);
-            acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[i], xh, acc[j][i], 0, 0, 0);
-          }
+            for (int pt = 0; pt < PARTS; ++pt) x[s][j][pt] = ahead[s][j][pt];
+        // the next units' rows of x, while these are multiplied
+        if (s0 + PF < kUnits) load_x(it, s0 + PF);
+        else if (it + 1 < i1) load_x(it + 1, 0);
+#pragma unroll
+        for (int s = 0; s < PF; ++s) {
+          half8 hi[R], lo[R];
+#pragma unroll
+          for (int i = 0; i < R; ++i) decode8<LO>(now[i][(s0 + s) / 2], (s0 + s) % 2, tb[i], hi[i], lo[i]);
+#pragma unroll
+          for (int j = 0; j < JJ; ++j)
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              if constexpr (LO) acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo[i], x[s][j][0], acc[j][i], 0, 0, 0);
+              if constexpr (PARTS == 2)
+                acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[i], x[s][j][PARTS - 1], acc[j][i], 0, 0, 0);
+              acc[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi[i], x[s][j][0], acc[j][i], 0, 0, 0);
+            }
         }
+        __builtin_amdgcn_sched_barrier(0);  // loads of later units moved up here would spill
       }
     }
   }
@@ -417,7 +509,7 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
   __shared__ uint32_t tops[kTileM];
   const Tile tl = find_tile<kTileT>(a.offsets, a.experts, a.t, blockIdx.y);
   if (tl.rows == 0) return;
-  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
   const int r = lane % 32, q = lane / 32, rw = wave / 2, cw = wave % 2, cpg = chunks_per_group(n);
   const int chunks = a.groups * cpg;
   const int64_t units = padded_chunks(n, a.groups) * kUnits;
@@ -446,7 +538,7 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
       for (int k = 0; k < SU / 4; ++k) {
         const int u = 4 * k + wave / 2, c = (wave % 2) * 64 + lane;
         const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
-        load_to_lds(frags + ((u0 + u + pt * 2 * units) * a.t + row) * 8, &xs[buf][pt][u][(wave % 2) * 64][0]);
+        load_to_lds(frags + (((u0 + u) * PARTS + pt) * a.t + row) * 8, &xs[buf][pt][u][(wave % 2) * 64][0]);
       }
   };
   uint4_t next[2];
@@ -624,7 +716,7 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
   __shared__ float xscale[TT];
   const Tile tl = find_tile<TT>(a.offsets, a.experts, a.t, blockIdx.y);
   if (tl.rows == 0) return;
-  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = tid / 64, r = lane % 16, q = lane / 16;
+  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64), r = lane % 16, q = lane / 16;
   int id = blockIdx.x;
   const int wblk = id % pl.per_group;
   id /= pl.per_group;
@@ -793,36 +885,44 @@ __device__ __forceinline__ bool covered(const int64_t* offsets, int experts, int
   return offsets == nullptr || (row >= offsets[0] && row < offsets[experts]);
 }
 
-// zv = the sum of its parts; zeros for rows that no expert has (P takes rows in pairs, and what lies in a row's
-// neighbour may show in its last bits).
-__global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int splits, const float* parts, int64_t k, float* zv) {
-  const int64_t row = blockIdx.x, i = (static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x) * 4;
-  if (i >= k) return;
+// The sum of a row's parts at four columns (this factor's of part 0 at p, `stride` floats from part to part), by four
+// threads a quarter of the parts each; the sum is thread `sub` 0's.
+__device__ __forceinline__ float4_t sum_parts(const float* p, int64_t stride, int splits, int sub, float4_t (&lds)[4][64],
+                                              int at) {
   float4_t v = {0.f, 0.f, 0.f, 0.f};
-  if (covered(a.offsets, a.experts, row))
-    for (int s = 0; s < splits; ++s)
-      v += *reinterpret_cast<const float4_t*>(parts + ((static_cast<int64_t>(s) * 2 + 1) * a.t + row) * k + i);
-  *reinterpret_cast<float4_t*>(zv + row * k + i) = v;
+#pragma unroll 8
+  for (int s = sub; s < splits; s += 4) v += *reinterpret_cast<const float4_t*>(p + s * stride);
+  lds[sub][at] = v;
+  __syncthreads();
+  return lds[0][at] + lds[1][at] + lds[2][at] + lds[3][at];
+}
+
+// zv = the sum of its parts; zeros for rows that no expert has (P takes rows in pairs, and what lies in a row's
+// neighbour may show in its last bits).  256 columns a workgroup.
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int splits, const float* parts, int64_t k, float* zv) {
+  __shared__ float4_t lds[4][64];
+  const int at = threadIdx.x % 64, sub = threadIdx.x / 64;
+  const int64_t row = blockIdx.x, i = (static_cast<int64_t>(blockIdx.y) * 64 + at) * 4;
+  const bool has = covered(a.offsets, a.experts, row) && i < k;
+  const float4_t v = sum_parts(parts + (a.t + row) * k + (has ? i : 0), 2 * a.t * k, has ? splits : 0, sub, lds, at);
+  if (sub == 0 && i < k) *reinterpret_cast<float4_t*>(zv + row * k + i) = v;
 }
 
 // y = zu + P zv, zu the sum of its parts: into y, or as fp32 rows into z (the rotation follows).
 __global__ __launch_bounds__(256) void finish_kernel(ProductArgs a, int splits, const float* parts, const float* pz, int64_t k,
                                                      float* z) {
-  const int64_t row = blockIdx.x, i = (static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x) * 4;
-  if (i >= k) return;
-  float4_t v = {0.f, 0.f, 0.f, 0.f};
-  if (covered(a.offsets, a.experts, row)) {
-    for (int s = 0; s < splits; ++s)
-      v += *reinterpret_cast<const float4_t*>(parts + (static_cast<int64_t>(s) * 2 * a.t + row) * k + i);
-    v += *reinterpret_cast<const float4_t*>(pz + row * k + i);
-  } else if (z == nullptr) {
-    return;
-  }
+  __shared__ float4_t lds[4][64];
+  const int at = threadIdx.x % 64, sub = threadIdx.x / 64;
+  const int64_t row = blockIdx.x, i = (static_cast<int64_t>(blockIdx.y) * 64 + at) * 4;
+  const bool has = covered(a.offsets, a.experts, row) && i < k;
+  float4_t v = sum_parts(parts + row * k + (has ? i : 0), 2 * a.t * k, has ? splits : 0, sub, lds, at);
+  if (sub != 0 || i >= k || (!has && z == nullptr)) return;
+  if (has) v += *reinterpret_cast<const float4_t*>(pz + row * k + i);
   if (z != nullptr) {
     *reinterpret_cast<float4_t*>(z + row * k + i) = v;
   } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) put(a.y, a.y_dtype, row * a.ldy + i + j, v[j]);
+    const float o[4] = {v[0], v[1], v[2], v[3]};
+    put4(a.y, a.y_dtype, row * a.ldy + i, 4, o);
   }
 }
 
@@ -848,11 +948,12 @@ hipError_t widen(const ProductArgs& a, int64_t width, float* out, hipStream_t s)
   return hipGetLastError();
 }
 
-// out = P in, t rows of `groups` vectors
-hipError_t apply_p(const ProductArgs& a, const float* in, float* out, hipStream_t s) {
+// out = P in, t rows of `groups` vectors (of a row behind each other; rows apart only for one group)
+hipError_t apply_p(const ProductArgs& a, const XRows& in, float* out, hipStream_t s) {
   KArgs p = a.p;
-  p.w = in;
-  p.ldw = a.n;
+  p.w = in.p;
+  p.dtype = in.dtype;
+  p.ldw = a.groups == 1 ? in.ld : a.n;
   p.m = a.t * a.groups;
   p.y = out;
   p.ldy = a.n;
@@ -867,29 +968,35 @@ template <int J, int R, bool LO>
 hipError_t launch_rows(const ProductArgs& a, const _Float16* frags, const int32_t* exps, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((a.m + 16 * R - 1) / (16 * R)),
                   static_cast<unsigned>(most_tiles(a.offsets != nullptr, a.t, a.experts, tile_rows<J>())));
-  hipLaunchKernelGGL((rows_kernel<J, R, LO>), grid, dim3(kRowsT), 0, s, a, frags, exps);
+  if (a.n % (kChunk * kSlab) == 0) hipLaunchKernelGGL((rows_kernel<J, R, LO, true>), grid, dim3(kRowsT), 0, s, a, frags, exps);
+  else hipLaunchKernelGGL((rows_kernel<J, R, LO, false>), grid, dim3(kRowsT), 0, s, a, frags, exps);
   return hipGetLastError();
 }
 
 // Rows of x that a matrix (an expert's, on average) meets.
 int64_t rows_each(int64_t t, int experts) { return t / (experts < t ? experts : t > 0 ? t : 1); }
 
-ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts) {
+// The number of splits goes by the sizes alone (the workspace does not know y's type); the tile by both.
+ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, bool grouped, bool lo) {
   ColumnsPlan p;
   const int64_t each = rows_each(t, experts);
-  p.j = each <= 8 ? 0 : each <= 16 ? 1 : 2;
-  p.steps = 16;
-  const int units = (n + 255) / 256 * (16 / p.steps);
-  for (p.waves = 8; p.waves > 1; p.waves /= 2)  // at most an eighth of the waves idle
-    if (((units + p.waves - 1) / p.waves * p.waves - units) * 8 <= units) break;
-  p.per_group = (units + p.waves - 1) / p.waves;
-  p.tiles = most_tiles(experts > 1, t, experts, p.j == 0 ? 8 : 16 * p.j);
-  // enough workgroups to fill the chip twice over, of at least 64 rows each
+  auto geometry = [&](int j, int steps) {
+    p.j = j;
+    p.steps = steps;
+    const int units = (n + 255) / 256 * (16 / steps);
+    for (p.waves = 8; p.waves > 1; p.waves /= 2)  // at most an eighth of the waves idle
+      if (((units + p.waves - 1) / p.waves * p.waves - units) * 8 <= units) break;
+    p.per_group = (units + p.waves - 1) / p.waves;
+    p.tiles = most_tiles(grouped, t, experts, j == 0 ? 8 : 16 * j);
+  };
+  geometry(each <= 8 ? 0 : each <= 16 ? 1 : 2, 16);
+  // enough workgroups of eight waves to fill the chip twice over, of at least 64 rows each
   const int64_t one = static_cast<int64_t>(p.per_group) * groups * 2 * (p.tiles > 0 ? p.tiles : 1);
   const int64_t want = (512 * 8 / p.waves + one - 1) / one, most = (m + 63) / 64;
-  int64_t splits = want < most ? want : most;
+  const int64_t splits = want < most ? want : most;
   p.rows = ((m + splits - 1) / splits + 31) / 32 * 32;
   p.splits = static_cast<int>((m + p.rows - 1) / p.rows);
+  if (!lo) geometry(each <= 16 ? 1 : each <= 32 ? 2 : 4, each <= 32 ? 16 : 8);
   return p;
 }
 
@@ -920,7 +1027,8 @@ hipError_t launch_columns(const ProductArgs& a, const ColumnsPlan& p, const floa
 
 hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   const int64_t k = static_cast<int64_t>(a.groups) * a.n;
-  const ColumnsPlan p = plan_columns(a.n, a.m, a.groups, a.t, a.experts);
+  const bool lo = a.y_dtype != KASHIN_BF16;  // as the rows' product
+  const ColumnsPlan p = plan_columns(a.n, a.m, a.groups, a.t, a.experts, a.offsets != nullptr, lo);
   const ColumnsWork at = columns_work(p, a.n, a.m, a.groups, a.t, a.experts);
   float* x = reinterpret_cast<float*>(a.work + at.x);
   int32_t* exps = reinterpret_cast<int32_t*>(a.work + at.exps);
@@ -938,14 +1046,19 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   };
   hipError_t e = a.x_dtype == KASHIN_E4M3 ? scale(e4m3_t()) : with_float_type(a.x_dtype, scale);
   if (e != hipSuccess) return e;
-  e = p.j == 0   ? launch_columns<0, 16, true>(a, p, x, exps, tops, parts, s)
-      : p.j == 1 ? launch_columns<1, 16, true>(a, p, x, exps, tops, parts, s)
-                 : launch_columns<2, 16, true>(a, p, x, exps, tops, parts, s);
+  if (lo)
+    e = p.j == 0   ? launch_columns<0, 16, true>(a, p, x, exps, tops, parts, s)
+        : p.j == 1 ? launch_columns<1, 16, true>(a, p, x, exps, tops, parts, s)
+                   : launch_columns<2, 16, true>(a, p, x, exps, tops, parts, s);
+  else
+    e = p.j == 1   ? launch_columns<1, 16, false>(a, p, x, exps, tops, parts, s)
+        : p.j == 2 ? launch_columns<2, 16, false>(a, p, x, exps, tops, parts, s)
+                   : launch_columns<4, 8, false>(a, p, x, exps, tops, parts, s);
   if (e != hipSuccess) return e;
-  const dim3 whole(static_cast<unsigned>(a.t), static_cast<unsigned>((k + 1023) / 1024));
+  const dim3 whole(static_cast<unsigned>(a.t), static_cast<unsigned>((k + 255) / 256));
   hipLaunchKernelGGL(join_kernel, whole, dim3(256), 0, s, a, p.splits, parts, k, zv);
   e = hipGetLastError();
-  if (e == hipSuccess) e = apply_p(a, zv, pz, s);
+  if (e == hipSuccess) e = apply_p(a, {zv, k, KASHIN_F32}, pz, s);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(finish_kernel, whole, dim3(256), 0, s, a, p.splits, parts, pz, k, a.rot ? zv : nullptr);
   e = hipGetLastError();
@@ -962,30 +1075,46 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
 int64_t product_workspace_bytes(int n, int64_t m, int groups, int64_t t, int experts, bool back) {
   const int64_t k = static_cast<int64_t>(groups) * n;
   if (t == 0) return 0;
-  if (back) return columns_work(plan_columns(n, m, groups, t, experts), n, m, groups, t, experts).end;
+  if (back) return columns_work(plan_columns(n, m, groups, t, experts, experts > 1, true), n, m, groups, t, experts).end;
   return 2 * align256(t * k * 4) + align256(t * 4) + 4 * padded_chunks(n, groups) * kUnits * t * 16;
 }
 
 hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
   if (a.back) return product_back(a, s);
   const int64_t k = static_cast<int64_t>(a.groups) * a.n;
-  float* x = reinterpret_cast<float*>(a.work);
+  float* wide = reinterpret_cast<float*>(a.work);
   float* px = reinterpret_cast<float*>(a.work + align256(a.t * k * 4));
   int32_t* exps = reinterpret_cast<int32_t*>(a.work + 2 * align256(a.t * k * 4));
   _Float16* frags = reinterpret_cast<_Float16*>(a.work + 2 * align256(a.t * k * 4) + align256(a.t * 4));
   // bf16 results are rounded by 2^-9 each; operands rounded to fp16 (2^-12) add nothing to speak of
   const int64_t each = rows_each(a.t, a.experts);
-  const bool lo = each <= 16 || a.y_dtype != KASHIN_BF16;
-  hipError_t e = widen(a, k, x, s);
-  if (e == hipSuccess && a.rot) e = rotate(a, false, x, s);
+  const bool lo = a.y_dtype != KASHIN_BF16;
+  const int parts = lo ? 2 : 1;
+  // the caller's rows where P can read them, else fp32 ones
+  XRows x = {a.x, a.ldx, a.x_dtype};
+  hipError_t e = hipSuccess;
+  if (a.x_dtype == KASHIN_E4M3 || (a.groups > 1 && a.ldx != k)) {
+    e = widen(a, k, wide, s);
+    x = {wide, k, KASHIN_F32};
+  }
+  if (e == hipSuccess && a.rot) {
+    // rows of one group may lie apart, groups of a row lie behind each other
+    e = launch_rotate(a.n, a.rot_seed, false, x.p, x.dtype, a.groups == 1 ? x.ld : a.n, wide, a.n, a.t * a.groups, s);
+    x = {wide, k, KASHIN_F32};
+  }
   if (e == hipSuccess) e = apply_p(a, x, px, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(split_rows_kernel, dim3(static_cast<unsigned>(a.t)), dim3(kSplitT), 0, s, x, px, a.n, a.groups, a.t, lo,
-                     frags, exps);
+
+  if (a.t >= 64)
+    hipLaunchKernelGGL((split_rows_kernel<8>), dim3(static_cast<unsigned>((a.t + 7) / 8)), dim3(kSplitT), 0, s, x, px, a.n,
+                       a.groups, a.t, parts, frags, exps);
+  else
+    hipLaunchKernelGGL((split_rows_kernel<1>), dim3(static_cast<unsigned>(a.t)), dim3(kSplitT), 0, s, x, px, a.n, a.groups, a.t,
+                       parts, frags, exps);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (each <= 8) return launch_rows<0, 1, true>(a, frags, exps, s);
-  if (each <= 16) return launch_rows<1, 1, true>(a, frags, exps, s);
+  if (each <= 8 && lo) return launch_rows<0, 1, true>(a, frags, exps, s);
+  if (each <= 16) return lo ? launch_rows<1, 1, true>(a, frags, exps, s) : launch_rows<1, 1, false>(a, frags, exps, s);
   // enough tiles of 256 x 128 to fill the chip
   if (each >= 96 && ((a.m + kTileM - 1) / kTileM) * (a.t / kTileT) >= 128) {
     const dim3 grid(static_cast<unsigned>((a.m + kTileM - 1) / kTileM),

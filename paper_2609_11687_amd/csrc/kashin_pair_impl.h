@@ -1754,7 +1754,8 @@ __global__ __launch_bounds__(C::T) __attribute__((amdgpu_waves_per_eu(C::W))) vo
 // buffer, in row order, so codes are read one byte per four elements and w_hat is written in
 // contiguous 16-byte vectors; y = P x loads and stores in the register layout directly
 // (measured faster for it than staging).
-template <class C, bool ROT, bool GROUPED>
+// IT: the element type of y = P x's rows (fp16 and bf16 for rows of activations; these instances take no codes).
+template <class C, bool ROT, bool GROUPED, class IT = float>
 __global__ __launch_bounds__(C::T) __attribute__((amdgpu_waves_per_eu(C::W))) void pair_pmap_kernel(
     KArgs ka, int64_t item0, int64_t nitems) {
   __shared__ __align__(16) float2 lds[C::LDS + small_tw_total<C>()];
@@ -1791,7 +1792,7 @@ __global__ __launch_bounds__(C::T) __attribute__((amdgpu_waves_per_eu(C::W))) vo
   const float qnan = __int_as_float(0x7fc00000);
   float* lf = reinterpret_cast<float*>(lds);  // staging: row a at [0, N), row b at [N, 2N)
   float4* lf4 = reinterpret_cast<float4*>(lds);
-  const bool recon = a.mode == MODE_RECON;
+  const bool recon = std::is_same<IT, float>::value && a.mode == MODE_RECON;
   const bool vout = (reinterpret_cast<uintptr_t>(a.y) % 16 == 0) && (a.ldy % 4 == 0);
   for (int64_t it = first; it < nitems; it += stride) {
     const int64_t ra = 2 * (item0 + it);
@@ -1814,7 +1815,7 @@ __global__ __launch_bounds__(C::T) __attribute__((amdgpu_waves_per_eu(C::W))) vo
     // 1. y = P x reads its rows straight into the register layout; the reconstruction decodes
     // the v codes in row order into LDS (row b zero when absent)
     if (!recon) {
-      load_pair<C>(z, a.w, /*fp32*/ 0, a.ldw, ra, rb, tid);
+      load_pair_t<C>(z, static_cast<const IT*>(a.w), a.ldw, ra, rb, tid);
     } else {
       const float* cea = a.in_centers + ra * 8 + 4;
       const float* ceb = a.in_centers + (rb >= 0 ? rb : ra) * 8 + 4;
@@ -2343,6 +2344,10 @@ hipError_t launch_cfg(const KArgs& a, int64_t grid, hipStream_t s) {
         if constexpr (rot_fusable(C::N))
           hipLaunchKernelGGL((pair_pmap_kernel<C, true, false>), dim3(static_cast<unsigned>(pg)), bd, 0, s, a, i0, g);
       } else if (a.ngroup > 0) hipLaunchKernelGGL((pair_pmap_kernel<C, false, true>), dim3(static_cast<unsigned>(pg)), bd, 0, s, a, i0, g);
+      else if (a.mode == MODE_APPLY_P && a.dtype == KASHIN_F16)
+        hipLaunchKernelGGL((pair_pmap_kernel<C, false, false, __half>), dim3(static_cast<unsigned>(pg)), bd, 0, s, a, i0, g);
+      else if (a.mode == MODE_APPLY_P && a.dtype == KASHIN_BF16)
+        hipLaunchKernelGGL((pair_pmap_kernel<C, false, false, bf16_t>), dim3(static_cast<unsigned>(pg)), bd, 0, s, a, i0, g);
       else hipLaunchKernelGGL((pair_pmap_kernel<C, false, false>), dim3(static_cast<unsigned>(pg)), bd, 0, s, a, i0, g);
     }
     const hipError_t e = hipGetLastError();
