@@ -705,7 +705,7 @@ __global__ __launch_bounds__(kScaleT) void scale_columns_kernel(const T* x, int6
 // `rows` matrix rows (a multiple of 32), of which there are `splits` per matrix; their sums are joined afterwards.
 struct ColumnsPlan {
   int j, steps, waves, per_group, splits;
-  int64_t rows, tiles;
+  int64_t rows, tiles, part_rows;
 };
 
 template <int J, int STEPS, bool LO>
@@ -991,11 +991,15 @@ ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, b
   };
   geometry(each <= 8 ? 0 : each <= 16 ? 1 : 2, 16);
   // enough workgroups of eight waves to fill the chip twice over, of at least 64 rows each
-  const int64_t one = static_cast<int64_t>(p.per_group) * groups * 2 * (p.tiles > 0 ? p.tiles : 1);
-  const int64_t want = (512 * 8 / p.waves + one - 1) / one, most = (m + 63) / 64;
-  const int64_t splits = want < most ? want : most;
+  const int64_t fill = 512 * 8 / p.waves, one = static_cast<int64_t>(p.per_group) * groups * 2;
+  const int64_t tiles = p.tiles > 0 ? p.tiles : 1, most = (m + 63) / 64;
+  const int64_t want = (fill + one * tiles - 1) / (one * tiles), splits = want < most ? want : most;
   p.rows = ((m + splits - 1) / splits + 31) / 32 * 32;
   p.splits = static_cast<int>((m + p.rows - 1) / p.rows);
+  // splits * t of this and of every smaller t (a workspace for t rows serves fewer): at most one split a 64 rows, and
+  // tiles of at most 32 rows each want their share of `fill`
+  const int64_t bound = (fill / one + 1) * 32 + t;
+  p.part_rows = most * t < bound ? most * t : bound;
   if (!lo) geometry(each <= 16 ? 1 : each <= 32 ? 2 : 4, each <= 32 ? 16 : 8);
   return p;
 }
@@ -1012,7 +1016,7 @@ ColumnsWork columns_work(const ColumnsPlan& p, int n, int64_t m, int groups, int
   w.zv = w.tops + align256(static_cast<int64_t>(experts) * kTopSlices * 4);
   w.pz = w.zv + align256(t * k * 4);
   w.parts = w.pz + align256(t * k * 4);
-  w.end = w.parts + static_cast<int64_t>(p.splits) * 2 * t * k * 4;
+  w.end = w.parts + p.part_rows * 2 * k * 4;
   return w;
 }
 

@@ -481,35 +481,60 @@ def kashin_optq_quantize_noalloc(plan, w_t, u, v, chunk, exact, lloyd_iters, cod
 
 
 # ----------------------------------------------------------------------------- a quantised model's layers
+_row_codes = None
+
+
 def _float_codes():
-    import torch
-    return {torch.float32: KASHIN_F32, torch.float16: KASHIN_F16, torch.bfloat16: KASHIN_BF16}
+    """KASHIN codes of the rows' dtypes (e4m3 among them)."""
+    global _row_codes
+    if _row_codes is None:
+        import torch
+        _row_codes = {torch.float32: KASHIN_F32, torch.float16: KASHIN_F16, torch.bfloat16: KASHIN_BF16,
+                      torch.float8_e4m3fn: KASHIN_E4M3}
+    return _row_codes
 
 
-def _need_float_rows(t, name, device, width=None, rows=None, e4m3=False):
-    """(rows, leading dimension, dtype code) of a 2-D tensor with unit-stride rows on `device`."""
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch tensor")
+def _where(t):
+    return t.get_device() if t.is_cuda else None
+
+
+def _need_float_rows(t, name, index, width, rows, e4m3=False):
+    """(leading dimension, dtype code) of a rows x width tensor with unit-stride rows on cuda:index."""
     code = _float_codes().get(t.dtype)
-    if code is None and e4m3 and t.dtype == torch.float8_e4m3fn:
-        code = KASHIN_E4M3
-    if code is None:
+    if code is None or (code == KASHIN_E4M3 and not e4m3):
         raise TypeError(f"{name} has unsupported dtype {t.dtype}")
-    m, ld = _rows(t)
-    if (width is not None and t.shape[1] != width) or (rows is not None and m != rows):
-        raise ValueError(f"{name} must have shape {(rows if rows is not None else m, width)} (got {tuple(t.shape)})")
-    if m and (t.device.type != "cuda" or t.device != device):
-        raise ValueError(f"{name} must live on {device if device.type == 'cuda' else 'a cuda device'} (got {t.device})")
-    return m, ld, code
+    if t.shape != (rows, width):
+        raise ValueError(f"{name} must have shape {(rows, width)} (got {tuple(t.shape)})")
+    if not rows:
+        return width, code
+    if not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{name} must live on {'a cuda device' if index is None else f'cuda:{index}'} (got {t.device})")
+    ld, unit = t.stride()
+    if unit != 1 and width > 1:
+        raise ValueError(f"{name} must have unit-stride rows")
+    return (width if rows == 1 else ld), code  # one row: its stride is never used
 
 
-def _stream_on(device, stream):
-    """`stream`, or the current one of `device` (a tensor's, which need not be the current device)."""
-    if stream is not None:
-        return _stream(stream)
+def _need_flat(t, name, index, shape, dtype):
+    """The address of a contiguous tensor of `shape` and `dtype` on cuda:index."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if not t.is_cuda or t.get_device() != index:
+        if t.numel():
+            raise ValueError(f"{name} must live on {'a cuda device' if index is None else f'cuda:{index}'} (got {t.device})")
+    return t.data_ptr()
+
+
+def _stream_on(index, stream):
+    """`stream`'s handle, or that of the current one of cuda:index (which need not be the current device)."""
     import torch
-    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    if stream is None:
+        return torch.cuda.current_stream(index).cuda_stream
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def kashin_rmsnorm(x, residual, weight, eps, h, y, scales=None, group=0, stream=None):
@@ -517,30 +542,36 @@ def kashin_rmsnorm(x, residual, weight, eps, h, y, scales=None, group=0, stream=
     x, residual, weight, h: one dtype (fp32, fp16, bf16); y: fp32, fp16, bf16, or float8_e4m3fn with
     scales (t x ceil(n / group) fp32, contiguous; t x 1 for group 0)."""
     import torch
-    t, ldx, code = _need_float_rows(x, "x", x.device)
-    n = x.shape[1]
-    _, ldy, y_code = _need_float_rows(y, "y", x.device, n, t, e4m3=True)
+    if x.dim() != 2:
+        raise ValueError(f"x must have two dimensions (got {tuple(x.shape)})")
+    (t, n), dtype, index = x.shape, x.dtype, _where(x)
+    ldx, code = _need_float_rows(x, "x", index, n, t)
+    ldy, y_code = _need_float_rows(y, "y", index, n, t, True)
     ldr = ldh = n
-    for name, v in (("residual", residual), ("h", h), ("weight", weight)):
-        if v is not None and v.dtype != x.dtype:
-            raise TypeError(f"{name} must be {x.dtype} (got {v.dtype})")
+    pr = ph = pw = ps = None
+    for name, v in (("residual", residual), ("weight", weight), ("h", h)):
+        if v is not None and v.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype} (got {v.dtype})")
     if residual is not None:
-        _, ldr, _ = _need_float_rows(residual, "residual", x.device, n, t)
+        ldr, _ = _need_float_rows(residual, "residual", index, n, t)
+        pr = residual.data_ptr()
     if h is not None:
-        _, ldh, _ = _need_float_rows(h, "h", x.device, n, t)
-    if weight is not None and (tuple(weight.shape) != (n,) or not weight.is_contiguous() or
-                               (t and weight.device != x.device)):
-        raise ValueError(f"weight must be {n} contiguous entries on {x.device}")
+        ldh, _ = _need_float_rows(h, "h", index, n, t)
+        ph = h.data_ptr()
+    if weight is not None:
+        pw = _need_flat(weight, "weight", index, (n,), dtype)
     if scales is not None:
         if group < 0:
             raise ValueError("group must be >= 0")
-        _need(None, scales, (t, -(-n // group) if group else 1), torch.float32, "scales")
-        if t and scales.device != x.device:
-            raise ValueError(f"scales must live on {x.device}")
-    with torch.cuda.device(x.device if t else -1):
-        _check(lib().kashin_rmsnorm(t, n, _ptr(x), code, ldx, _ptr(residual), ldr, _ptr(weight), eps, _ptr(h), ldh,
-                                    _ptr(y), y_code, ldy, _ptr(scales), group,
-                                    _stream_on(x.device, stream) if t else None))
+        ps = _need_flat(scales, "scales", index, (t, -(-n // group) if group else 1), torch.float32)
+    args = (t, n, x.data_ptr(), code, ldx, pr, ldr, pw, eps, ph, ldh, y.data_ptr(), y_code, ldy, ps, group)
+    if not t:
+        _check(lib().kashin_rmsnorm(*args, None))
+    elif index == torch.cuda.current_device():
+        _check(lib().kashin_rmsnorm(*args, _stream_on(index, stream)))
+    else:
+        with torch.cuda.device(index):
+            _check(lib().kashin_rmsnorm(*args, _stream_on(index, stream)))
 
 
 class Weights(ctypes.Structure):
@@ -557,32 +588,35 @@ def kashin_matmul_workspace_bytes(n, m, groups, t, experts=1, transposed=False) 
 def _matmul(name, plan, codes_u, codes_v, centers, x, y, work, x_scales, x_group, rot_seed, stream, transposed,
             offsets=None):
     import torch
-    wide, narrow = (y, x) if transposed else (x, y)  # k and m columns
-    if x.dim() != 2 or y.dim() != 2 or wide.shape[1] % plan.n or not wide.shape[1]:
-        raise ValueError(f"{'y' if transposed else 'x'} must have a multiple of {plan.n} columns "
-                         f"(got {tuple(wide.shape)})")
-    groups, m = wide.shape[1] // plan.n, narrow.shape[1]
+    if x.dim() != 2 or y.dim() != 2:
+        raise ValueError("x and y must have two dimensions")
+    (t, wx), wy, n, index = x.shape, y.shape[1], plan.n, plan.device
+    k, m = (wy, wx) if transposed else (wx, wy)
+    if not k or k % n:
+        raise ValueError(f"{'y' if transposed else 'x'} must have a multiple of {n} columns (got {k})")
+    groups = k // n
     experts = 1 if offsets is None else offsets.numel() - 1
-    device = torch.device("cuda", plan.device)
-    t, ldx, x_code = _need_float_rows(x, "x", device, e4m3=True)
-    _, ldy, y_code = _need_float_rows(y, "y", device, rows=t, width=y.shape[1])
-    _need_codes(plan, experts * m * groups, codes_u, codes_v, centers)
+    ldx, x_code = _need_float_rows(x, "x", index, wx, t, True)
+    ldy, y_code = _need_float_rows(y, "y", index, wy, t)
+    rows, u8, f32 = experts * m * groups, torch.uint8, torch.float32
+    w = Weights(plan.handle, None, _need_flat(codes_u, "codes_u", index, (rows, (n + 3) // 4), u8),
+                _need_flat(codes_v, "codes_v", index, (rows, (n + 3) // 4), u8),
+                _need_flat(centers, "centers", index, (rows, 2, 4), f32), m, groups, experts)
+    more = ()
     if offsets is not None:
-        _need(plan, offsets, (experts + 1,), torch.int64, "offsets")
+        more = (_need_flat(offsets, "offsets", index, (experts + 1,), torch.int64), 1 if transposed else 0)
+    ps = None
     if x_scales is not None:
         if x_group < 0:
             raise ValueError("x_group must be >= 0")
-        _need(plan, x_scales, (t, -(-x.shape[1] // x_group) if x_group else 1), torch.float32, "x_scales")
-    if work.dtype != torch.uint8 or work.dim() != 1 or (work.numel() and not work.is_contiguous()):
-        raise ValueError("work must be a contiguous 1-D uint8 tensor")
-    if work.numel():
-        _on_plan_device(plan, work, "work")
-    seed = None if rot_seed is None else ctypes.c_uint64(rot_seed)
-    w = Weights(plan.handle, None if seed is None else ctypes.addressof(seed), codes_u.data_ptr(), codes_v.data_ptr(),
-                centers.data_ptr(), m, groups, experts)
-    more = () if offsets is None else (_ptr(offsets), 1 if transposed else 0)
-    _check(getattr(lib(), name)(ctypes.addressof(w), *more, _ptr(x), x_code, t, ldx, _ptr(x_scales), x_group, _ptr(y),
-                                y_code, ldy, _ptr(work), work.numel(), _stream_on(device, stream) if t else None))
+        ps = _need_flat(x_scales, "x_scales", index, (t, -(-wx // x_group) if x_group else 1), f32)
+    size = work.numel()
+    pwork = _need_flat(work, "work", index, (size,), u8)
+    if rot_seed is not None:
+        seed = ctypes.c_uint64(rot_seed)
+        w.rot_seed = ctypes.addressof(seed)
+    _check(getattr(lib(), name)(ctypes.addressof(w), *more, x.data_ptr(), x_code, t, ldx, ps, x_group, y.data_ptr(), y_code,
+                                ldy, pwork, size, _stream_on(index, stream) if t else None))
 
 
 def kashin_matmul(plan, codes_u, codes_v, centers, x, y, work, x_scales=None, x_group=0, rot_seed=None, stream=None):

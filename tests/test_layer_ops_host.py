@@ -56,11 +56,12 @@ def test_workspace_sizes_refused(args):
     assert K.lib().kashin_matmul_workspace_bytes(*args) == -1
 
 
-def test_workspace_sizes_grow_with_the_rows():
-    for back in (False, True):
-        sizes = [K.kashin_matmul_workspace_bytes(4096, 11008, 1, t, 1, back) for t in (0, 1, 2, 17, 300, 4000, 65536)]
-        assert sizes[0] >= 0 and sizes == sorted(sizes)
-        assert K.kashin_matmul_workspace_bytes(4096, 11008, 1, 300, 8, back) >= sizes[4]
+@pytest.mark.parametrize("n,m,groups,experts", [(4096, 11008, 1, 1), (512, 100, 2, 1), (11008, 4096, 1, 1), (64, 5000, 9, 1),
+                                                (256, 64, 16, 1), (4096, 2048, 1, 8), (2048, 1000, 1, 64)])
+@pytest.mark.parametrize("back", [False, True])
+def test_workspace_for_more_rows_serves_fewer(n, m, groups, experts, back):
+    sizes = [K.kashin_matmul_workspace_bytes(n, m, groups, t, experts, back) for t in list(range(700)) + [4000, 40000, 65536]]
+    assert sizes[0] >= 0 and sizes == sorted(sizes)
 
 
 def test_binding_checks_before_calling():
