@@ -704,6 +704,7 @@ __global__ __launch_bounds__(kScaleT) void scale_columns_kernel(const T* x, int6
 // The split of a transposed product: a workgroup of `waves` waves takes as many blocks of columns of one group, over
 // `rows` matrix rows (a multiple of 32), of which there are `splits` per matrix; their sums are joined afterwards.
 struct ColumnsPlan {
+  bool tiled;  // columns_tile_kernel: a workgroup takes 256 columns of a group
   int j, steps, waves, per_group, splits;
   int64_t rows, tiles, part_rows;
 };
@@ -880,6 +881,224 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
   }
 }
 
+// y = x W for many rows of x: a workgroup computes 128 rows of x by 256 columns of a factor over a range of matrix rows,
+// wave (cw, tw) 64 by 64 of them in 32 x 32 tiles, 32 matrix rows at a time.  The workgroup decodes the 32 x 256 codes once,
+// a dword a thread, into LDS as fp16 rows; operand B takes them with loads that transpose (a lane wants one column of
+// eight matrix rows).  A dword's codes lie in LDS in the order they come out of the tables, 0 4 8 12 1 5 9 13 ..: column
+// 16 d + p / 4 + 4 (p % 4) at place p, which the stores undo.
+// x comes as units of eight matrix rows: units[part][unit][row of x][8], scaled as for x W^T.
+constexpr int kColsM = 32, kColsN = 256, kColsT = 128, kColsLd = kColsN + 32;  // 576-byte rows: four of them on 64 banks
+using short4_t = short __attribute__((ext_vector_type(4)));
+
+__host__ __device__ inline int64_t column_units(int64_t m) { return (m + kColsM - 1) / kColsM * (kColsM / 8); }
+
+constexpr int kUnitRows = 8;
+template <class T>
+__global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int64_t ldx, const float* scales, int group, int64_t m,
+                                                                int64_t t, int parts, const float* centers, int64_t per_expert,
+                                                                _Float16* units, int32_t* exps, uint32_t* tops) {
+  __shared__ uint32_t top_of[kUnitRows];
+  const int tid = threadIdx.x, mine = tid % kUnitRows;
+  const int64_t row_blocks = (t + kUnitRows - 1) / kUnitRows;
+  if (tid < kUnitRows) top_of[tid] = 0;
+  __syncthreads();
+  uint32_t top = 0;
+  if (blockIdx.x >= row_blocks) {  // the largest finite centre of a slice of an expert's
+    const int64_t id = blockIdx.x - row_blocks, e = id / kTopSlices, slice = id % kTopSlices;
+    const float* ce = centers + e * per_expert;
+    for (int64_t i = (slice * kSplitT + tid) * 4; i < per_expert; i += kTopSlices * kSplitT * 4) {
+      const float4_t v = *reinterpret_cast<const float4_t*>(ce + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
+        top = b > top && b < kInfBits ? b : top;
+      }
+    }
+    if (top) atomicMax(&top_of[0], top);  // a maximum: the same in any order
+    __syncthreads();
+    if (tid == 0) tops[id] = top_of[0];
+    return;
+  }
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kUnitRows + mine;
+  const bool real = row < t;
+  auto load_unit = [&](int64_t u, float (&v)[8]) {
+    const int64_t i = 8 * u, left = m - i;
+    load8(x + (real ? row * ldx + i : 0), real ? (left < 8 ? static_cast<int>(left < 0 ? 0 : left) : 8) : 0, v);
+    if (scales != nullptr && real && left > 0) {
+      const float s = group ? scales[row * ((m + group - 1) / group) + i / group] : scales[row];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = j < left ? v[j] * s : 0.f;
+    }
+  };
+  const int64_t all = column_units(m);
+  for (int64_t u = tid / kUnitRows; u < all; u += kSplitT / kUnitRows) {
+    float v[8];
+    load_unit(u, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t o = __float_as_uint(v[j]) & 0x7fffffffu;
+      top = o > top ? o : top;
+    }
+  }
+  if (top) atomicMax(&top_of[mine], top);
+  __syncthreads();
+  top = top_of[mine];
+  const bool bad = top >= kInfBits;
+  const int e = bad ? 0 : scale_exponent(top);
+  const float scale = bad ? __int_as_float(0x7fc00000) : power_of_two(e);
+  if (!real) return;
+  if (tid < kUnitRows) exps[row] = e;
+  for (int64_t u = tid / kUnitRows; u < all; u += kSplitT / kUnitRows) {
+    float v[8];
+    load_unit(u, v);
+    half8 h, l;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float w = v[j] * scale;
+      h[j] = static_cast<_Float16>(w);
+      l[j] = static_cast<_Float16>(w - static_cast<float>(h[j]));
+    }
+    *reinterpret_cast<half8*>(units + (u * t + row) * 8) = h;
+    if (parts == 2) *reinterpret_cast<half8*>(units + ((all + u) * t + row) * 8) = l;
+  }
+}
+
+template <bool LO>
+__global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, ColumnsPlan pl, const _Float16* units,
+                                                              const int32_t* exps, const uint32_t* tops, float* out) {
+  constexpr int PARTS = LO ? 2 : 1;
+  __shared__ __align__(16) _Float16 ws[2][PARTS][kColsM][kColsLd];
+  __shared__ __align__(16) _Float16 xs[2][PARTS][kColsM / 8][kColsT][8];
+  __shared__ int32_t ex[kColsT];
+  const Tile tl = find_tile<kColsT>(a.offsets, a.experts, a.t, blockIdx.y);
+  if (tl.rows == 0) return;
+  const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
+  const int r = lane % 32, q = lane / 32, cw = wave / 2, tw = wave % 2;
+  int id = blockIdx.x;
+  const int block = id % pl.per_group;
+  id /= pl.per_group;
+  const int g = id % a.groups;
+  id /= a.groups;
+  const int f = id % 2, split = id / 2;
+  const int64_t i0 = split * pl.rows, i1 = i0 + pl.rows < a.m ? i0 + pl.rows : a.m;
+  uint32_t top = 0;
+#pragma unroll
+  for (int s = 0; s < kTopSlices; ++s) {
+    const uint32_t o = tops[tl.expert * kTopSlices + s];
+    top = o > top ? o : top;
+  }
+  const int ec = scale_exponent(top);
+  const float cscale = power_of_two(ec);
+  if (tid < kColsT) ex[tid] = tid < tl.rows ? exps[tl.row0 + tid] : 0;
+  // this thread's dword of codes: matrix row `mine` of a step, columns 16 d ..; past a group's last byte its last four
+  // are read and moved down
+  const int mine = tid / 16, d = tid % 16;
+  int off = block * 64 + 4 * d, shift = 0;
+  if (off > nby - 4) {
+    shift = 8 * (off - (nby - 4));
+    shift = shift < 24 ? shift : 24;
+    off = nby - 4;
+  }
+  const uint8_t* codes = f ? a.codes_v : a.codes_u;
+  uint32_t w;
+  float4_t ce;
+  auto load_codes_of = [&](int64_t k0) {
+    const int64_t i = k0 + mine, row = (tl.expert * a.m + (i < a.m ? i : a.m - 1)) * a.groups + g;
+    __builtin_memcpy(&w, codes + row * nby + off, 4);
+    ce = *reinterpret_cast<const float4_t*>(a.centers + row * 8 + 4 * f);
+  };
+  auto decode = [&](int buf) {
+    const Table tb = make_table(ce, cscale);
+    w >>= shift;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      half8 hi, lo;
+      decode8<LO>(w, h, tb, hi, lo);
+      *reinterpret_cast<half8*>(&ws[buf][0][mine][16 * d + 8 * h]) = hi;
+      if constexpr (LO) *reinterpret_cast<half8*>(&ws[buf][PARTS - 1][mine][16 * d + 8 * h]) = lo;
+    }
+  };
+  const int64_t all = column_units(a.m);
+  auto fill = [&](int64_t k0, int buf) {
+    const int c = (wave % 2) * 64 + lane, u = wave / 2;
+    const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
+#pragma unroll
+    for (int pt = 0; pt < PARTS; ++pt)
+      load_to_lds(units + ((pt * all + k0 / 8 + u) * a.t + row) * 8, &xs[buf][pt][u][(wave % 2) * 64][0]);
+  };
+  float16_t acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
+  fill(i0, 0);
+  load_codes_of(i0);
+  decode(0);
+  wait_lds_loads();
+  __syncthreads();
+  // the lane's place in a transposing load: matrix row (lane / 32) 8 + lane % 16 / 4 of sixteen, four columns
+  const int tr_row = (lane / 32) * 8 + (lane % 16) / 4, tr_col = 64 * cw + (lane / 16 % 2) * 16 + 4 * (lane % 4);
+  int buf = 0;
+  for (int64_t k0 = i0; k0 < i1; k0 += kColsM, buf ^= 1) {
+    const bool more = k0 + kColsM < i1;
+    if (more) {
+      fill(k0 + kColsM, buf ^ 1);
+      load_codes_of(k0 + kColsM);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      half8 x[2][PARTS], b[2][PARTS];
+#pragma unroll
+      for (int pt = 0; pt < PARTS; ++pt) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          x[i][pt] = *reinterpret_cast<const half8*>(&xs[buf][pt][2 * ks + q][64 * tw + 32 * i + r][0]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          union {
+            short4_t s[2];
+            half8 h;
+          } v;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            v.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) short4_t*)&ws[buf][pt][16 * ks + 4 * h + tr_row][tr_col + 32 * j]);
+          b[j][pt] = v.h;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if constexpr (LO) {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], b[j][PARTS - 1], acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][PARTS - 1], b[j][0], acc[i][j], 0, 0, 0);
+          }
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], b[j][0], acc[i][j], 0, 0, 0);
+        }
+    }
+    if (more) decode(buf ^ 1);
+    wait_lds_loads();
+    __syncthreads();
+  }
+  const int64_t k = static_cast<int64_t>(a.groups) * n;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int c = 64 * tw + 32 * i + 8 * (v / 4) + 4 * q + v % 4;
+      if (c >= tl.rows) continue;
+      float* o = out + ((static_cast<int64_t>(split) * 2 + f) * a.t + tl.row0 + c) * k + static_cast<int64_t>(g) * n;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int place = 64 * cw + 32 * j + r, col = block * kColsN + place / 16 * 16 + place % 16 / 4 + 4 * (place % 4);
+        if (col < n) o[col] = ldexpf(acc[i][j][v], -(ec + ex[c]));
+      }
+    }
+}
+
 // Whether a row belongs to an expert (all do without offsets).
 __device__ __forceinline__ bool covered(const int64_t* offsets, int experts, int64_t row) {
   return offsets == nullptr || (row >= offsets[0] && row < offsets[experts]);
@@ -1000,7 +1219,19 @@ ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, b
   // tiles of at most 32 rows each want their share of `fill`
   const int64_t bound = (fill / one + 1) * 32 + t;
   p.part_rows = most * t < bound ? most * t : bound;
-  if (!lo) geometry(each <= 16 ? 1 : each <= 32 ? 2 : 4, each <= 32 ? 16 : 8);
+  p.tiled = each >= 48;
+  if (p.tiled) {
+    p.per_group = (n + kColsN - 1) / kColsN;
+    p.tiles = most_tiles(grouped, t, experts, kColsT);
+    // two workgroups a compute unit, of at least 256 matrix rows each; never more than the bound above, whose tiles
+    // are a quarter of these and whose workgroups take 2048 columns
+    const int64_t others = static_cast<int64_t>(p.per_group) * groups * 2 * p.tiles;
+    const int64_t wanted = (512 + others - 1) / others, top = (m + 255) / 256, cut = wanted < top ? wanted : top;
+    p.rows = ((m + cut - 1) / cut + 31) / 32 * 32;
+    p.splits = static_cast<int>((m + p.rows - 1) / p.rows);
+  } else if (!lo) {
+    geometry(each <= 16 ? 1 : each <= 32 ? 2 : 4, each <= 32 ? 16 : 8);
+  }
   return p;
 }
 
@@ -1011,7 +1242,7 @@ ColumnsWork columns_work(const ColumnsPlan& p, int n, int64_t m, int groups, int
   const int64_t k = static_cast<int64_t>(groups) * n;
   ColumnsWork w;
   w.x = 0;
-  w.exps = w.x + align256(t * m * 4);
+  w.exps = w.x + align256(t * column_units(m) * 32);  // fp32 rows, or units in two parts
   w.tops = w.exps + align256(t * 4);
   w.zv = w.tops + align256(static_cast<int64_t>(experts) * kTopSlices * 4);
   w.pz = w.zv + align256(t * k * 4);
@@ -1040,24 +1271,37 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   float* zv = reinterpret_cast<float*>(a.work + at.zv);
   float* pz = reinterpret_cast<float*>(a.work + at.pz);
   float* parts = reinterpret_cast<float*>(a.work + at.parts);
-  const dim3 grid(static_cast<unsigned>(a.t + static_cast<int64_t>(a.experts) * kTopSlices));
-  const int64_t per_expert = a.m * a.groups * 8;
+  _Float16* units = reinterpret_cast<_Float16*>(a.work + at.x);
+  const int64_t per_expert = a.m * a.groups * 8, slices = static_cast<int64_t>(a.experts) * kTopSlices;
   auto scale = [&](auto zero) {
     using T = decltype(zero);
-    hipLaunchKernelGGL((scale_columns_kernel<T>), grid, dim3(kScaleT), 0, s, static_cast<const T*>(a.x), a.ldx, a.x_scales,
-                       a.x_group, a.m, a.t, a.centers, per_expert, x, exps, tops);
+    const T* rows = static_cast<const T*>(a.x);
+    if (p.tiled)
+      hipLaunchKernelGGL((split_columns_kernel<T>), dim3(static_cast<unsigned>((a.t + kUnitRows - 1) / kUnitRows + slices)),
+                         dim3(kSplitT), 0, s, rows, a.ldx, a.x_scales, a.x_group, a.m, a.t, lo ? 2 : 1, a.centers, per_expert,
+                         units, exps, tops);
+    else
+      hipLaunchKernelGGL((scale_columns_kernel<T>), dim3(static_cast<unsigned>(a.t + slices)), dim3(kScaleT), 0, s, rows, a.ldx,
+                         a.x_scales, a.x_group, a.m, a.t, a.centers, per_expert, x, exps, tops);
     return hipGetLastError();
   };
   hipError_t e = a.x_dtype == KASHIN_E4M3 ? scale(e4m3_t()) : with_float_type(a.x_dtype, scale);
   if (e != hipSuccess) return e;
-  if (lo)
+  if (p.tiled) {
+    const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.per_group) * a.groups * 2 * p.splits),
+                    static_cast<unsigned>(p.tiles));
+    if (lo) hipLaunchKernelGGL((columns_tile_kernel<true>), grid, dim3(512), 0, s, a, p, units, exps, tops, parts);
+    else hipLaunchKernelGGL((columns_tile_kernel<false>), grid, dim3(512), 0, s, a, p, units, exps, tops, parts);
+    e = hipGetLastError();
+  } else if (lo) {
     e = p.j == 0   ? launch_columns<0, 16, true>(a, p, x, exps, tops, parts, s)
         : p.j == 1 ? launch_columns<1, 16, true>(a, p, x, exps, tops, parts, s)
                    : launch_columns<2, 16, true>(a, p, x, exps, tops, parts, s);
-  else
+  } else {
     e = p.j == 1   ? launch_columns<1, 16, false>(a, p, x, exps, tops, parts, s)
         : p.j == 2 ? launch_columns<2, 16, false>(a, p, x, exps, tops, parts, s)
                    : launch_columns<4, 8, false>(a, p, x, exps, tops, parts, s);
+  }
   if (e != hipSuccess) return e;
   const dim3 whole(static_cast<unsigned>(a.t), static_cast<unsigned>((k + 255) / 256));
   hipLaunchKernelGGL(join_kernel, whole, dim3(256), 0, s, a, p.splits, parts, k, zv);
