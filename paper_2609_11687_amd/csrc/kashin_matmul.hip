@@ -495,14 +495,20 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
 using float16_t = float __attribute__((ext_vector_type(16)));
 constexpr int kTileM = 256, kTileT = 128;
 
-// Loads to LDS of this wave have arrived (a barrier alone does not wait for them).
-__device__ __forceinline__ void wait_lds_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ void load_to_lds(const void* from, void* lds) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+// 16 bytes a lane from memory to LDS, lane by lane behind `lds` (the same in all lanes).  Written as an instruction: the
+// compiler would let every later LDS read wait for it, also of the other buffer.  It has no register output; who reads the
+// data waits with wait_loads first, then at a barrier (which alone does not wait).
+__device__ __forceinline__ void load_to_lds(const void* from, const void* lds) {
+  const int at = uniform(static_cast<int>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)lds)));
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(at) : "memory", "m0");
+}
+// Until at most N of this wave's loads are under way (they arrive in order).
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-template <bool LO>
+template <bool LO, bool ALIGNED>
 __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const _Float16* frags, const int32_t* exps) {
   constexpr int PARTS = LO ? 2 : 1, SU = 2 * kUnits;  // units of a slab: two chunks
   __shared__ __align__(16) _Float16 xs[2][PARTS][SU][kTileT][8];
@@ -510,49 +516,62 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
   const Tile tl = find_tile<kTileT>(a.offsets, a.experts, a.t, blockIdx.y);
   if (tl.rows == 0) return;
   const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
-  const int r = lane % 32, q = lane / 32, rw = wave / 2, cw = wave % 2, cpg = chunks_per_group(n);
-  const int chunks = a.groups * cpg;
-  const int64_t units = padded_chunks(n, a.groups) * kUnits;
-  const int slabs = (chunks + 1) / 2, items = 2 * slabs;
-  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTileM;
-  int64_t first[2];
+  const int r = lane % 32, q = lane / 32, rw = wave / 2, cw = wave % 2, cpg = chunks_per_group(n), groups = a.groups;
+  const int chunks = groups * cpg;
+  const int64_t units = padded_chunks(n, groups) * kUnits;
+  const int slabs = (chunks + 1) / 2, items = 2 * slabs, per_group = cpg / 2;  // per_group: ALIGNED
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTileM, matrix0 = (tl.expert * a.m + row0) * groups;
+  uint32_t crow[2];  // this lane's matrix rows (past the last repeat it), as offsets from the workgroup's first
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int64_t row = row0 + 64 * rw + 32 * i + r;
-    first[i] = (tl.expert * a.m + (row < a.m ? row : a.m - 1)) * a.groups;
+    const int64_t left = a.m - 1 - row0;
+    const int at = 64 * rw + 32 * i + r;
+    crow[i] = static_cast<uint32_t>((at < left ? at : left) * groups);
   }
+  const uint8_t* cu = a.codes_u + matrix0 * nby;
+  const uint8_t* cv = a.codes_v + matrix0 * nby;
+  const float* ce = a.centers + matrix0 * 8;
   auto load_item = [&](int it, uint4_t (&c)[2]) {
-    const int f = it >= slabs, chunk = (it - f * slabs) * 2 + q;
-    const uint8_t* base = f ? a.codes_v : a.codes_u;
-    const int at = chunk < chunks ? chunk : chunks - 1;
-    const int g = a.groups == 1 ? 0 : at / cpg, off = (at - g * cpg) * 16;
+    const int f = it >= slabs, slab = it - f * slabs;
+    const uint8_t* base = f ? cv : cu;
+    if constexpr (ALIGNED) {
+      base += slab * 32;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) c[i] = load_codes(base + (first[i] + g) * nby, nby, off);
+      for (int i = 0; i < 2; ++i)
+        __builtin_memcpy(&c[i], base + static_cast<uint32_t>(crow[i] * static_cast<uint32_t>(nby) + 16 * q), 16);
+    } else {
+      const int chunk = slab * 2 + q, at = chunk < chunks ? chunk : chunks - 1, g = at / cpg;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        c[i] = load_codes(base + static_cast<uint32_t>((crow[i] + g) * static_cast<uint32_t>(nby)), nby, (at - g * cpg) * 16);
+    }
   };
   auto fill = [&](int it, int buf) {
-    const int f = it >= slabs;
+    const int f = it >= slabs, c = (wave % 2) * 64 + lane;
     const int64_t u0 = f * units + static_cast<int64_t>(it - f * slabs) * SU;
+    const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
 #pragma unroll
     for (int pt = 0; pt < PARTS; ++pt)
 #pragma unroll
       for (int k = 0; k < SU / 4; ++k) {
-        const int u = 4 * k + wave / 2, c = (wave % 2) * 64 + lane;
-        const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
+        const int u = 4 * k + wave / 2;
         load_to_lds(frags + (((u0 + u) * PARTS + pt) * a.t + row) * 8, &xs[buf][pt][u][(wave % 2) * 64][0]);
       }
   };
-  uint4_t next[2];
-  load_item(0, next);
+  // codes are loaded two items ahead: an item takes less time than memory does
+  uint4_t next[2][2];
+  load_item(0, next[0]);
   fill(0, 0);
+  load_item(1, next[1]);  // items is even
   if (tid < kTileM) tops[tid] = 0;
   __syncthreads();
   {
     uint32_t top = 0;
     const int mine = tid % kTileM;
-    const int64_t row = row0 + mine;
-    const float* ce = a.centers + (tl.expert * a.m + (row < a.m ? row : a.m - 1)) * a.groups * 8;
-    for (int64_t j = tid / kTileM; j < a.groups * 2; j += 512 / kTileM) {
-      const float4_t v = *reinterpret_cast<const float4_t*>(ce + 4 * j);
+    const int64_t left = a.m - 1 - row0;
+    const float* mc = ce + static_cast<uint32_t>((mine < left ? mine : left) * groups) * 8u;
+    for (int j = tid / kTileM; j < groups * 2; j += 512 / kTileM) {
+      const float4_t v = *reinterpret_cast<const float4_t*>(mc + 4 * j);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t b = __float_as_uint(v[k]) & 0x7fffffffu;
@@ -561,7 +580,7 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
     }
     if (top) atomicMax(&tops[mine], top);  // a maximum: the same in any order
   }
-  wait_lds_loads();
+  wait_loads<0>();
   __syncthreads();
   float scale[2];
 #pragma unroll
@@ -578,43 +597,54 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
       for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
   Table tb[2];
   int held = -1;
-  for (int it = 0; it < items; ++it) {
-    const int buf = it & 1, f = it >= slabs, chunk = (it - f * slabs) * 2 + q;
-    const int g = a.groups == 1 ? 0 : (chunk < chunks ? chunk : chunks - 1) / cpg;
-    uint4_t now[2] = {next[0], next[1]};
-    if (it + 1 < items) {
-      fill(it + 1, buf ^ 1);
-      load_item(it + 1, next);
-    }
-    if (f * a.groups + g != held) {
-      held = f * a.groups + g;
+  for (int b0 = 0; b0 < items; b0 += 2) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        tb[i] = make_table(*reinterpret_cast<const float4_t*>(a.centers + (first[i] + g) * 8 + 4 * f), scale[i]);
-    }
-#pragma unroll
-    for (int s = 0; s < kUnits; ++s) {
-      half8 hi[2], lo[2], xh[2], xl[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        xh[j] = *reinterpret_cast<const half8*>(&xs[buf][0][q * kUnits + s][64 * cw + 32 * j + r][0]);
-        if constexpr (LO) xl[j] = *reinterpret_cast<const half8*>(&xs[buf][1][q * kUnits + s][64 * cw + 32 * j + r][0]);
+    for (int buf = 0; buf < 2; ++buf) {  // items is even
+      const int it = b0 + buf, f = it >= slabs, slab = it - f * slabs;
+      int g;
+      if constexpr (ALIGNED) {
+        g = groups == 1 ? 0 : slab / per_group;
+      } else {
+        const int chunk = slab * 2 + q;
+        g = (chunk < chunks ? chunk : chunks - 1) / cpg;
       }
+      uint4_t now[2] = {next[buf][0], next[buf][1]};
+      // taken before the loads to LDS are issued: the compiler counts its own loads only, and would wait for those too
+      asm volatile("" : "+v"(now[0]), "+v"(now[1]));
+      fill(it + 1 < items ? it + 1 : it, buf ^ 1);  // past the last item: what nobody reads
+      if (f * groups + g != held) {
+        held = f * groups + g;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) decode8<LO>(now[i][s / 2], s % 2, tb[i], hi[i], lo[i]);
+        for (int i = 0; i < 2; ++i)
+          tb[i] = make_table(*reinterpret_cast<const float4_t*>(ce + 8 * g + 4 * f + static_cast<uint32_t>(crow[i] * 8)), scale[i]);
+      }
+      load_item(it + 2 < items ? it + 2 : items - 1, next[buf]);
+      __builtin_amdgcn_sched_barrier(0);  // issued here, not behind the products
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int s = 0; s < kUnits; ++s) {
+        half8 hi[2], lo[2], xh[2], xl[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          if constexpr (LO) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo[i], xh[j], acc[i][j], 0, 0, 0);
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi[i], xl[j], acc[i][j], 0, 0, 0);
-          }
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi[i], xh[j], acc[i][j], 0, 0, 0);
+          xh[j] = *reinterpret_cast<const half8*>(&xs[buf][0][q * kUnits + s][64 * cw + 32 * j + r][0]);
+          if constexpr (LO) xl[j] = *reinterpret_cast<const half8*>(&xs[buf][1][q * kUnits + s][64 * cw + 32 * j + r][0]);
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) decode8<LO>(now[i][s / 2], s % 2, tb[i], hi[i], lo[i]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if constexpr (LO) {
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo[i], xh[j], acc[i][j], 0, 0, 0);
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi[i], xl[j], acc[i][j], 0, 0, 0);
+            }
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi[i], xh[j], acc[i][j], 0, 0, 0);
+          }
+      }
+      // x of the next item has arrived when at most the two loads of codes behind it are under way
+      wait_loads<ALIGNED ? 2 : 0>();
+      __syncthreads();
     }
-    wait_lds_loads();
-    __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -1000,20 +1030,22 @@ __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, Col
     off = nby - 4;
   }
   const uint8_t* codes = f ? a.codes_v : a.codes_u;
-  uint32_t w;
-  float4_t ce;
-  auto load_codes_of = [&](int64_t k0) {
+  // codes and centres are loaded three steps ahead: a step takes less time than memory does
+  constexpr int AHEAD = 3;
+  uint32_t w[AHEAD];
+  float4_t ce[AHEAD];
+  auto load_codes_of = [&](int64_t k0, int at) {
     const int64_t i = k0 + mine, row = (tl.expert * a.m + (i < a.m ? i : a.m - 1)) * a.groups + g;
-    __builtin_memcpy(&w, codes + row * nby + off, 4);
-    ce = *reinterpret_cast<const float4_t*>(a.centers + row * 8 + 4 * f);
+    __builtin_memcpy(&w[at], codes + row * nby + off, 4);
+    ce[at] = *reinterpret_cast<const float4_t*>(a.centers + row * 8 + 4 * f);
   };
-  auto decode = [&](int buf) {
-    const Table tb = make_table(ce, cscale);
-    w >>= shift;
+  auto decode = [&](int buf, uint32_t codes_of, float4_t centers_of) {
+    const Table tb = make_table(centers_of, cscale);
+    const uint32_t word = codes_of >> shift;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       half8 hi, lo;
-      decode8<LO>(w, h, tb, hi, lo);
+      decode8<LO>(word, h, tb, hi, lo);
       *reinterpret_cast<half8*>(&ws[buf][0][mine][16 * d + 8 * h]) = hi;
       if constexpr (LO) *reinterpret_cast<half8*>(&ws[buf][PARTS - 1][mine][16 * d + 8 * h]) = lo;
     }
@@ -1033,20 +1065,29 @@ __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, Col
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
+  const int steps = static_cast<int>((i1 - i0 + kColsM - 1) / kColsM);
   fill(i0, 0);
-  load_codes_of(i0);
-  decode(0);
-  wait_lds_loads();
+#pragma unroll
+  for (int e = 0; e < AHEAD; ++e) load_codes_of(i0 + e * kColsM, e);  // past the last row: that row again
+  decode(0, w[0], ce[0]);
+  wait_loads<0>();
   __syncthreads();
   // the lane's place in a transposing load: matrix row (lane / 32) 8 + lane % 16 / 4 of sixteen, four columns
   const int tr_row = (lane / 32) * 8 + (lane % 16) / 4, tr_col = 64 * cw + (lane / 16 % 2) * 16 + 4 * (lane % 4);
-  int buf = 0;
-  for (int64_t k0 = i0; k0 < i1; k0 += kColsM, buf ^= 1) {
-    const bool more = k0 + kColsM < i1;
-    if (more) {
-      fill(k0 + kColsM, buf ^ 1);
-      load_codes_of(k0 + kColsM);
-    }
+  for (int s0 = 0; s0 < steps; s0 += AHEAD) {
+#pragma unroll
+   for (int e = 0; e < AHEAD; ++e) {
+    const int st = s0 + e, buf = st & 1;
+    if (st >= steps) break;
+    const int64_t k0 = i0 + static_cast<int64_t>(st) * kColsM;
+    // the next step's codes, taken before the loads to LDS are issued: the compiler counts its own loads only, and would
+    // wait for those too
+    uint32_t codes_of = w[(e + 1) % AHEAD];
+    float4_t centers_of = ce[(e + 1) % AHEAD];
+    asm volatile("" : "+v"(codes_of), "+v"(centers_of));
+    fill(st + 1 < steps ? k0 + kColsM : k0, buf ^ 1);  // past the last step: what nobody reads
+    load_codes_of(k0 + AHEAD * kColsM, e);
+    __builtin_amdgcn_sched_barrier(0);  // issued here, not behind the products
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       half8 x[2][PARTS], b[2][PARTS];
@@ -1079,9 +1120,11 @@ __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, Col
           acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][0], b[j][0], acc[i][j], 0, 0, 0);
         }
     }
-    if (more) decode(buf ^ 1);
-    wait_lds_loads();
+    decode(buf ^ 1, codes_of, centers_of);
+    // x of the next step has arrived when at most the loads behind it, of codes and of centres, are under way
+    wait_loads<2>();
     __syncthreads();
+   }
   }
   const int64_t k = static_cast<int64_t>(a.groups) * n;
 #pragma unroll
@@ -1367,8 +1410,11 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
   if (each >= 96 && ((a.m + kTileM - 1) / kTileM) * (a.t / kTileT) >= 128) {
     const dim3 grid(static_cast<unsigned>((a.m + kTileM - 1) / kTileM),
                     static_cast<unsigned>(most_tiles(a.offsets != nullptr, a.t, a.experts, kTileT)));
-    if (lo) hipLaunchKernelGGL((rows_tile_kernel<true>), grid, dim3(512), 0, s, a, frags, exps);
-    else hipLaunchKernelGGL((rows_tile_kernel<false>), grid, dim3(512), 0, s, a, frags, exps);
+    const bool aligned = a.n % (kChunk * kSlab) == 0;
+    if (lo && aligned) hipLaunchKernelGGL((rows_tile_kernel<true, true>), grid, dim3(512), 0, s, a, frags, exps);
+    else if (lo) hipLaunchKernelGGL((rows_tile_kernel<true, false>), grid, dim3(512), 0, s, a, frags, exps);
+    else if (aligned) hipLaunchKernelGGL((rows_tile_kernel<false, true>), grid, dim3(512), 0, s, a, frags, exps);
+    else hipLaunchKernelGGL((rows_tile_kernel<false, false>), grid, dim3(512), 0, s, a, frags, exps);
     return hipGetLastError();
   }
   if (lo) return each <= 32 ? launch_rows<2, 2, true>(a, frags, exps, s) : launch_rows<4, 2, true>(a, frags, exps, s);
