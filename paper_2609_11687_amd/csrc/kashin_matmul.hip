@@ -25,6 +25,24 @@ __device__ __forceinline__ int64_t uniform(int64_t v) {
   return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
 }
 
+// The largest value of a wave, the same in all lanes (an atomic maximum of 64 lanes on one address would go through them
+// one by one).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t max_with(uint32_t v) {
+  const uint32_t o = static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(static_cast<int>(v), static_cast<int>(v), CTRL, ROWS, 0xf, false));
+  return o > v ? o : v;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max_with<0xb1, 0xf>(v);   // lanes 1 apart in fours
+  v = max_with<0x4e, 0xf>(v);   // 2 apart
+  v = max_with<0x141, 0xf>(v);  // halves of a row of 16 mirrored
+  v = max_with<0x140, 0xf>(v);  // rows mirrored
+  v = max_with<0x142, 0xa>(v);  // row 0 into 1, 2 into 3
+  v = max_with<0x143, 0xc>(v);  // rows 0, 1 into 2, 3
+  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 63));
+}
+
 // Tile number `tile` of at most TT rows that belong to one expert, tiles counted over the experts in turn; rows 0
 // past the last tile.  Every lane of the wave calls it.
 struct Tile {
@@ -275,10 +293,14 @@ __global__ __launch_bounds__(kSplitT) void split_rows_kernel(XRows x, const floa
       top = o > top ? o : top;
     }
   }
+  if constexpr (ROWS == 1) {
+    top = wave_max(top);
+  } else {
 #pragma unroll
-  for (int d = ROWS; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_xor(top, d);
-    top = o > top ? o : top;
+    for (int d = ROWS; d < 64; d <<= 1) {
+      const uint32_t o = __shfl_xor(top, d);
+      top = o > top ? o : top;
+    }
   }
   if (tid % 64 < ROWS) atomicMax(&tops[mine], top);  // a maximum: the same in any order
   __syncthreads();
@@ -390,27 +412,52 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
               half8, __builtin_amdgcn_raw_buffer_load_b128(units, col[j], ((s0 + s) * STORED + pt) * t * 16, 0));
   };
   if (i0 < i1) load_x(i0, 0);
-  // the scale of every matrix row: its largest centre over all groups
-  if (tid < 16 * R) tops[tid] = 0;
-  __syncthreads();
-  {
+  // the scale of every matrix row: its largest centre over all groups.  With one group a lane holds its rows' centres
+  // from the start, and nothing waits for the other waves.
+  float scale[R];
+  constexpr bool OWN = R == 1;  // where registers allow
+  float4_t own[R][2];
+  if (OWN && groups == 1) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        own[i][h] = *reinterpret_cast<const float4_t*>(ce + 4 * h + static_cast<uint32_t>(crow[i] * 8));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t b = __float_as_uint(own[i][h][c]) & 0x7fffffffu;
+          top = b > top ? b : top;
+        }
+      }
+      scale[i] = top >= kInfBits ? __int_as_float(0x7fc00000) : power_of_two(scale_exponent(top));
+      if (wave == 0 && q == 0) tops[16 * i + r] = top;  // for the sums, behind a barrier
+    }
+  } else {
+    if (tid < 16 * R) tops[tid] = 0;
+    __syncthreads();
     uint32_t top = 0;
     const int mine = tid % (16 * R);
     const int64_t left = a.m - 1 - row0;
     const float* mc = ce + static_cast<uint32_t>((mine < left ? mine : left) * groups) * 8u;
-    for (int j = tid / (16 * R); j < groups * 8; j += kRowsT / (16 * R)) {
-      const uint32_t b = __float_as_uint(mc[j]) & 0x7fffffffu;
-      top = b > top ? b : top;
+    for (int j = tid / (16 * R); j < groups * 2; j += kRowsT / (16 * R)) {
+      const float4_t v = *reinterpret_cast<const float4_t*>(mc + 4 * j);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t b = __float_as_uint(v[c]) & 0x7fffffffu;
+        top = b > top ? b : top;
+      }
     }
     if (top) atomicMax(&tops[mine], top);  // a maximum: the same in any order
-  }
-  __syncthreads();
-  float scale[R];
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < R; ++i) {
-    const uint32_t top = tops[16 * i + r];
-    scale[i] = top >= kInfBits ? __int_as_float(0x7fc00000) : power_of_two(scale_exponent(top));
+    for (int i = 0; i < R; ++i) {
+      top = tops[16 * i + r];
+      scale[i] = top >= kInfBits ? __int_as_float(0x7fc00000) : power_of_two(scale_exponent(top));
+    }
   }
+  // this thread's first sum's exponent of x, loaded early
+  const int xexp = exps[tl.row0 + (tid / (16 * R) < tl.rows ? tid / (16 * R) : 0)];
   float4_t acc[JJ][R];
 #pragma unroll
   for (int j = 0; j < JJ; ++j)
@@ -434,8 +481,10 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
       if (f * groups + g != held) {
         held = f * groups + g;
 #pragma unroll
-        for (int i = 0; i < R; ++i)
-          tb[i] = make_table(*reinterpret_cast<const float4_t*>(ce + 8 * g + 4 * f + static_cast<uint32_t>(crow[i] * 8)), scale[i]);
+        for (int i = 0; i < R; ++i) {
+          if (OWN && groups == 1) tb[i] = make_table(f ? own[i][1] : own[i][0], scale[i]);
+          else tb[i] = make_table(*reinterpret_cast<const float4_t*>(ce + 8 * g + 4 * f + static_cast<uint32_t>(crow[i] * 8)), scale[i]);
+        }
       }
       uint4_t now[R];
 #pragma unroll
@@ -485,7 +534,7 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
     for (int w = 0; w < NW; ++w) v += J == 0 ? sums[w][c][i] + sums[w][c + 8][i] : sums[w][c][i];
     const uint32_t top = tops[i];
     const int e = top >= kInfBits ? 0 : scale_exponent(top);
-    put(a.y, a.y_dtype, (tl.row0 + c) * a.ldy + row0 + i, ldexpf(v, -(e + exps[tl.row0 + c])));
+    put(a.y, a.y_dtype, (tl.row0 + c) * a.ldy + row0 + i, ldexpf(v, -(e + (o == tid ? xexp : exps[tl.row0 + c]))));
   }
 }
 
@@ -677,74 +726,40 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
 // 16-bit half, the halves masked by 0x0400, 0x0800 and 0x0c00 are the fp16 numbers b0, b1 and f times 2^-14: two codes
 // take a shift and three ands.
 //
-// Exponents of x's rows and the largest finite centres: x goes to fp32 with max |x| scaled into [2^6, 2^7), the centres
-// into [2^4, 2^5): a coefficient times x stays below 2^14.
-constexpr int kTopSlices = 16;  // partial maxima of an expert's centres
-constexpr int kScaleT = 256;
+// A workgroup scales by what it meets: max |x| of a row of x into [2^6, 2^7), the largest finite centre into [2^4, 2^5), so
+// that a coefficient times x stays below 2^14.
+constexpr int kTopSlices = 16;  // partial maxima of an expert's centres (the tiled kernel's)
+
+// The caller's rows of x.
 template <class T>
-__global__ __launch_bounds__(kScaleT) void scale_columns_kernel(const T* x, int64_t ldx, const float* scales, int group,
-                                                                int64_t width, int64_t t, const float* centers, int64_t per_expert,
-                                                                float* out, int32_t* exps, uint32_t* tops) {
-  __shared__ uint32_t part[kScaleT / 64];
-  uint32_t top = 0;
-  const int64_t row = blockIdx.x;
-  if (row < t) {
-    for (int64_t i = threadIdx.x * 8; i < width; i += kScaleT * 8) {
-      const int valid = width - i < 8 ? static_cast<int>(width - i) : 8;
-      float v[8];
-      load8(x + row * ldx + i, valid, v);
-      if (scales != nullptr) {
-        const float s = group ? scales[row * ((width + group - 1) / group) + i / group] : scales[row];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= s;
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
-        top = b > top && j < valid ? b : top;
-      }
-      store8(out + row * width + i, valid, v);
-    }
-  } else {
-    const int64_t e = (row - t) / kTopSlices, slice = (row - t) % kTopSlices;
-    const float* ce = centers + e * per_expert;
-    for (int64_t i = (slice * kScaleT + threadIdx.x) * 4; i < per_expert; i += kTopSlices * kScaleT * 4) {
-      const float4_t v = *reinterpret_cast<const float4_t*>(ce + i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
-        top = b > top && b < kInfBits ? b : top;  // a row that is not finite gives NaN by itself
-      }
-    }
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_xor(top, d);
-    top = o > top ? o : top;
-  }
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = top;
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-#pragma unroll
-  for (int w = 0; w < kScaleT / 64; ++w) top = part[w] > top ? part[w] : top;
-  if (row < t) exps[row] = top >= kInfBits ? 1024 : scale_exponent(top) - 7;  // 1024: the row is not finite
-  else tops[row - t] = top;
+struct XIn {
+  const T* p;
+  int64_t ld;
+  const float* scales;  // e4m3
+  int group, per_row;   // scales of a row
+};
+// Entry i of a row that starts `at` entries into p.
+template <class T>
+__device__ __forceinline__ float load1(const XIn<T>& x, int64_t at, int64_t row, uint32_t i) {
+  float v = widen(x.p[at + i]);
+  if constexpr (sizeof(T) == 1) v *= x.scales[row * x.per_row + (x.group ? i / static_cast<uint32_t>(x.group) : 0u)];
+  return v;
 }
 
 // The split of a transposed product: a workgroup of `waves` waves takes as many blocks of columns of one group, over
 // `rows` matrix rows (a multiple of 32), of which there are `splits` per matrix; their sums are joined afterwards.
 struct ColumnsPlan {
   bool tiled;  // columns_tile_kernel: a workgroup takes 256 columns of a group
-  int j, steps, waves, per_group, splits;
+  int j, waves, per_group, splits;
   int64_t rows, tiles, part_rows;
 };
 
-template <int J, int STEPS, bool LO>
-__global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsPlan pl, const float* x, const int32_t* exps,
-                                                         const uint32_t* tops, float* out) {
+template <int J, bool LO, class T>
+__global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsPlan pl, XIn<T> x, float* out) {
+  constexpr int STEPS = 16;  // columns of a lane's dword
   constexpr int TT = tile_rows<J>(), JJ = J == 0 ? 1 : J, PARTS = LO && J != 0 ? 2 : 1, CP = 16 * JJ;
   __shared__ __align__(16) _Float16 xs[2][4][PARTS][4][CP][8];  // [buffer][function][part][quarter][column of B][row]
-  __shared__ float xscale[TT];
+  __shared__ uint32_t tops[TT + 1];  // of the rows of x, of the centres
   const Tile tl = find_tile<TT>(a.offsets, a.experts, a.t, blockIdx.y);
   if (tl.rows == 0) return;
   const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64), r = lane % 16, q = lane / 16;
@@ -754,23 +769,10 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
   const int g = id % a.groups;
   id /= a.groups;
   const int f = id % 2, split = id / 2;
-  const int unit = wblk * pl.waves + wave, block = unit * STEPS / 16, half = STEPS == 16 ? 0 : unit % 2;
+  const int block = wblk * pl.waves + wave;
   const bool busy = block * 256 < n;
   const int64_t i0 = split * pl.rows, i1 = i0 + pl.rows < a.m ? i0 + pl.rows : a.m;
-  uint32_t top = 0;
-#pragma unroll
-  for (int s = 0; s < kTopSlices; ++s) {
-    const uint32_t o = tops[tl.expert * kTopSlices + s];
-    top = o > top ? o : top;
-  }
-  const int ec = scale_exponent(top) - 9;
-  const float cscale = power_of_two(ec);
-  for (int c = tid; c < TT; c += blockDim.x) {
-    const int e = c < tl.rows ? exps[tl.row0 + c] : 0;
-    xscale[c] = e == 1024 ? __int_as_float(0x7fc00000) : power_of_two(e);
-  }
-  __syncthreads();
-
+  const float* ce0 = a.centers + (tl.expert * a.m * a.groups + g) * 8 + 4 * f;  // of matrix row i: 8 groups i further
   const uint8_t* codes = f ? a.codes_v : a.codes_u;
   // the lane's dword of codes; at a group's end (n no multiple of 16, or past the last column) the last four bytes
   // are read and moved down
@@ -780,44 +782,106 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
     shift = shift < 24 ? shift : 24;
     off = nby - 4;
   }
+  // A step's codes through a buffer that ends with the expert's matrix (rows past the last come back as zeros): the lane's
+  // offsets stay in registers, a step moves the base.
+  const uint32_t stride = static_cast<uint32_t>(a.groups) * static_cast<uint32_t>(nby);  // of a matrix row
+  const uint8_t* codes0 = codes + (tl.expert * a.m * a.groups + g) * static_cast<int64_t>(nby);
+  uint32_t at[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) at[e] = (8 * q + e) * stride + off;
   auto load_codes8 = [&](int64_t k0, uint32_t (&w)[8]) {
+    const int64_t left = a.m > k0 ? (a.m - k0) * stride - static_cast<int64_t>(g) * nby : 0;
+    const auto rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(codes0) + k0 * stride, 0,
+                                                        left < 0x7fffffff ? static_cast<int>(left) : 0x7fffffff, 0x00027000);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int64_t i = k0 + 8 * q + e;
-      __builtin_memcpy(&w[e], codes + ((tl.expert * a.m + (i < a.m ? i : a.m - 1)) * a.groups + g) * nby + off, 4);
-    }
+    for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_raw_buffer_load_b32(rows, at[e], 0, 0);
   };
-  auto build = [&](int64_t k0, int buf) {
-    for (int it = tid; it < 16 * TT; it += blockDim.x) {
-      const int pair = it % 16, c = it / 16;
-      _Float16 h[2][4], l[2][4];
+  // Codes, and a thread's first item of operand B, are loaded AHEAD steps ahead: a step takes less time than memory does.
+  // Loads past the last matrix row take that row again.
+  // Item it = (it % 16, it / 16) = (pair of matrix rows, row of x).
+  constexpr int AHEAD = J <= 1 ? 3 : 1;
+  struct Item {
+    float x[2];
+    float4_t ce[2];
+  };
+  const uint32_t last = static_cast<uint32_t>(a.m - 1), cstride = static_cast<uint32_t>(a.groups) * 32u;
+  auto fetch = [&](int it, int64_t k0) {
+    Item v;
+    const int pair = it % 16, c = it / 16 < tl.rows ? it / 16 : tl.rows - 1;
+    const int64_t row = (tl.row0 + c) * x.ld;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int64_t i = k0 + 2 * pair + e;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (c < tl.rows && i < i1) {
-          const float4_t ce =
-              *reinterpret_cast<const float4_t*>(a.centers + ((tl.expert * a.m + i) * a.groups + g) * 8 + 4 * f) * cscale;
-          const float xv = x[(tl.row0 + c) * a.m + i] * xscale[c];
-          const float d = (ce[3] - ce[2]) - (ce[1] - ce[0]);
-          v[0] = xv * ce[0];
-          v[1] = xv * ((ce[1] - ce[0]) - d);
-          v[2] = xv * (0.5f * (ce[2] - ce[0]) - d);
-          v[3] = xv * d;
-        }
+    for (int e = 0; e < 2; ++e) {
+      uint32_t i = static_cast<uint32_t>(k0) + 2 * pair + e;
+      i = i < last ? i : last;
+      v.x[e] = load1(x, row, tl.row0 + c, i);
+      v.ce[e] = *reinterpret_cast<const float4_t*>(reinterpret_cast<const char*>(ce0) + static_cast<uint64_t>(i) * cstride);
+    }
+    return v;
+  };
+  for (int c = tid; c <= TT; c += blockDim.x) tops[c] = 0;
+  __syncthreads();
+  uint32_t next[AHEAD][8];
+  Item ahead[AHEAD];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          h[e][k] = static_cast<_Float16>(v[k]);
-          l[e][k] = static_cast<_Float16>(v[k] - static_cast<float>(h[e][k]));
-        }
+  for (int e = 0; e < AHEAD; ++e) {
+    load_codes8(i0 + 32 * e, next[e]);
+    ahead[e] = fetch(tid, i0 + 32 * e);
+  }
+  {
+    const int range = static_cast<int>(i1 - i0);
+    uint32_t top = 0;
+    for (int i = tid; i < range; i += blockDim.x) {
+      const float4_t v = *reinterpret_cast<const float4_t*>(ce0 + (i0 + i) * a.groups * 8);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
+        top = b > top && b < kInfBits ? b : top;  // a row that is not finite gives NaN by itself
       }
+    }
+    top = wave_max(top);
+    if (lane == 0) atomicMax(&tops[TT], top);  // a maximum: the same in any order
+    // a wave for each row of x in turn
+    for (int c = wave; c < tl.rows; c += blockDim.x / 64) {
+      top = 0;
+      for (int i = lane; i < range; i += 64) {
+        const uint32_t b = __float_as_uint(load1(x, (tl.row0 + c) * x.ld, tl.row0 + c, static_cast<uint32_t>(i0) + i)) & 0x7fffffffu;
+        top = b > top ? b : top;
+      }
+      top = wave_max(top);
+      if (lane == 0) tops[c] = top;
+    }
+  }
+  __syncthreads();
+  const int ec = scale_exponent(tops[TT]) - 9;
+  const float cscale = power_of_two(ec);
+  auto store = [&](int it, const Item& v, int64_t k0, int buf) {
+    const int pair = it % 16, c = it / 16;
+    const uint32_t top = tops[c];
+    const float xscale = top >= kInfBits ? __int_as_float(0x7fc00000) : power_of_two(scale_exponent(top) - 7);
+    _Float16 h[2][4], l[2][4];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float4_t ce = v.ce[e] * cscale;
+      const bool real = c < tl.rows && k0 + 2 * pair + e < i1;
+      const float xv = real ? v.x[e] * xscale : 0.f;
+      const float d = (ce[3] - ce[2]) - (ce[1] - ce[0]);
+      const float p[4] = {xv * ce[0], xv * ((ce[1] - ce[0]) - d), xv * (0.5f * (ce[2] - ce[0]) - d), xv * d};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        *reinterpret_cast<uint32_t*>(&xs[buf][k][0][pair / 4][c][2 * (pair % 4)]) = pair_bits(h[0][k], h[1][k]);
-        if constexpr (J == 0) *reinterpret_cast<uint32_t*>(&xs[buf][k][0][pair / 4][c + 8][2 * (pair % 4)]) = pair_bits(l[0][k], l[1][k]);
-        else if constexpr (LO) *reinterpret_cast<uint32_t*>(&xs[buf][k][PARTS - 1][pair / 4][c][2 * (pair % 4)]) = pair_bits(l[0][k], l[1][k]);
+        h[e][k] = static_cast<_Float16>(p[k]);
+        l[e][k] = static_cast<_Float16>(p[k] - static_cast<float>(h[e][k]));
       }
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      *reinterpret_cast<uint32_t*>(&xs[buf][k][0][pair / 4][c][2 * (pair % 4)]) = pair_bits(h[0][k], h[1][k]);
+      if constexpr (J == 0) *reinterpret_cast<uint32_t*>(&xs[buf][k][0][pair / 4][c + 8][2 * (pair % 4)]) = pair_bits(l[0][k], l[1][k]);
+      else if constexpr (LO) *reinterpret_cast<uint32_t*>(&xs[buf][k][PARTS - 1][pair / 4][c][2 * (pair % 4)]) = pair_bits(l[0][k], l[1][k]);
+    }
+  };
+  auto build = [&](const Item& first, int64_t k0, int buf) {
+    if (tid < 16 * TT) store(tid, first, k0, buf);
+    for (int it = tid + blockDim.x; it < 16 * TT; it += blockDim.x) store(it, fetch(it, k0), k0, buf);
   };
 
   float4_t acc[JJ][STEPS], flat[JJ];
@@ -827,19 +891,20 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) acc[j][s] = float4_t{0.f, 0.f, 0.f, 0.f};
   }
-  uint32_t next[8];
-  if (busy) load_codes8(i0, next);
-  build(i0, 0);
+  build(ahead[0], i0, 0);
   __syncthreads();
-  int buf = 0;
-  for (int64_t k0 = i0; k0 < i1; k0 += 32, buf ^= 1) {
+  const int steps = static_cast<int>((i1 - i0 + 31) / 32);
+  for (int s0 = 0; s0 < steps; s0 += AHEAD) {
+#pragma unroll
+   for (int e0 = 0; e0 < AHEAD; ++e0) {
+    const int st = s0 + e0, buf = st & 1;
+    if (st >= steps) break;
+    const int64_t k0 = i0 + static_cast<int64_t>(st) * 32;
     uint32_t w[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = next[e] >> shift;
-    if (k0 + 32 < i1) {
-      if (busy) load_codes8(k0 + 32, next);
-      build(k0 + 32, buf ^ 1);
-    }
+    for (int e = 0; e < 8; ++e) w[e] = next[e0][e] >> shift;
+    load_codes8(k0 + 32 * AHEAD, next[e0]);
+    ahead[e0] = fetch(tid, k0 + 32 * AHEAD);
     if (busy) {
       half8 b[JJ][4][PARTS];
 #pragma unroll
@@ -865,7 +930,7 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
         uint4_t fn[3];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t v = STEPS == 16 ? p[s / 8][e] : (half ? p[1][e] : p[0][e]);
+          const uint32_t v = p[s / 8][e];
           const int at = 2 * (s % 8);
           const uint32_t c = at <= 10 ? v << (10 - at) : v >> (at - 10);
           fn[0][e] = c & 0x04000400u;
@@ -881,7 +946,9 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
               acc[j][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, fn[k]), b[j][k + 1][pt], acc[j][s], 0, 0, 0);
       }
     }
+    build(ahead[(e0 + 1) % AHEAD], k0 + 32, buf ^ 1);  // past the last row: zeros that nobody reads
     __syncthreads();
+   }
   }
   if (!busy) return;
   const int64_t k = static_cast<int64_t>(a.groups) * n;
@@ -890,11 +957,12 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
     const int c = J == 0 ? r : 16 * j + r;
     const bool mine = c < tl.rows;
     const int64_t row = tl.row0 + (mine ? c : 0);
-    const int et = exps[row], unscale = 14 - ec - (et == 1024 ? 0 : et);
+    const uint32_t top = tops[mine ? c : 0];
+    const int unscale = 14 - ec - (top >= kInfBits ? 0 : scale_exponent(top) - 7);
     float* o = out + ((static_cast<int64_t>(split) * 2 + f) * a.t + row) * k + static_cast<int64_t>(g) * n;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int col = block * 256 + (4 * q + i) * 16 + half * 8;
+      const int col = block * 256 + (4 * q + i) * 16;
 #pragma unroll
       for (int s0 = 0; s0 < STEPS; s0 += 4) {
         float4_t v;
@@ -944,7 +1012,8 @@ __global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int6
         top = b > top && b < kInfBits ? b : top;
       }
     }
-    if (top) atomicMax(&top_of[0], top);  // a maximum: the same in any order
+    top = wave_max(top);
+    if (tid % 64 == 0) atomicMax(&top_of[0], top);  // a maximum: the same in any order
     __syncthreads();
     if (tid == 0) tops[id] = top_of[0];
     return;
@@ -1242,16 +1311,12 @@ int64_t rows_each(int64_t t, int experts) { return t / (experts < t ? experts : 
 ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, bool grouped, bool lo) {
   ColumnsPlan p;
   const int64_t each = rows_each(t, experts);
-  auto geometry = [&](int j, int steps) {
-    p.j = j;
-    p.steps = steps;
-    const int units = (n + 255) / 256 * (16 / steps);
-    for (p.waves = 8; p.waves > 1; p.waves /= 2)  // at most an eighth of the waves idle
-      if (((units + p.waves - 1) / p.waves * p.waves - units) * 8 <= units) break;
-    p.per_group = (units + p.waves - 1) / p.waves;
-    p.tiles = most_tiles(grouped, t, experts, j == 0 ? 8 : 16 * j);
-  };
-  geometry(each <= 8 ? 0 : each <= 16 ? 1 : 2, 16);
+  const int blocks = (n + 255) / 256;
+  for (p.waves = 8; p.waves > 1; p.waves /= 2)  // at most an eighth of the waves idle
+    if (((blocks + p.waves - 1) / p.waves * p.waves - blocks) * 8 <= blocks) break;
+  p.per_group = (blocks + p.waves - 1) / p.waves;
+  p.j = each <= 8 ? 0 : each <= 16 ? 1 : 2;
+  p.tiles = most_tiles(grouped, t, experts, p.j == 0 ? 8 : 16 * p.j);
   // enough workgroups of eight waves to fill the chip twice over, of at least 64 rows each
   const int64_t fill = 512 * 8 / p.waves, one = static_cast<int64_t>(p.per_group) * groups * 2;
   const int64_t tiles = p.tiles > 0 ? p.tiles : 1, most = (m + 63) / 64;
@@ -1272,8 +1337,9 @@ ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, b
     const int64_t wanted = (512 + others - 1) / others, top = (m + 255) / 256, cut = wanted < top ? wanted : top;
     p.rows = ((m + cut - 1) / cut + 31) / 32 * 32;
     p.splits = static_cast<int>((m + p.rows - 1) / p.rows);
-  } else if (!lo) {
-    geometry(each <= 16 ? 1 : each <= 32 ? 2 : 4, each <= 32 ? 16 : 8);
+  } else if (!lo && p.j == 0) {
+    p.j = 1;
+    p.tiles = most_tiles(grouped, t, experts, 16);
   }
   return p;
 }
@@ -1285,7 +1351,7 @@ ColumnsWork columns_work(const ColumnsPlan& p, int n, int64_t m, int groups, int
   const int64_t k = static_cast<int64_t>(groups) * n;
   ColumnsWork w;
   w.x = 0;
-  w.exps = w.x + align256(t * column_units(m) * 32);  // fp32 rows, or units in two parts
+  w.exps = w.x + align256(t * column_units(m) * 32);  // units in two parts
   w.tops = w.exps + align256(t * 4);
   w.zv = w.tops + align256(static_cast<int64_t>(experts) * kTopSlices * 4);
   w.pz = w.zv + align256(t * k * 4);
@@ -1294,12 +1360,18 @@ ColumnsWork columns_work(const ColumnsPlan& p, int n, int64_t m, int groups, int
   return w;
 }
 
-template <int J, int STEPS, bool LO>
-hipError_t launch_columns(const ProductArgs& a, const ColumnsPlan& p, const float* x, const int32_t* exps,
-                          const uint32_t* tops, float* parts, hipStream_t s) {
+template <int J, bool LO>
+hipError_t launch_columns(const ProductArgs& a, const ColumnsPlan& p, float* parts, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.per_group) * a.groups * 2 * p.splits),
                   static_cast<unsigned>(p.tiles));
-  hipLaunchKernelGGL((columns_kernel<J, STEPS, LO>), grid, dim3(64 * p.waves), 0, s, a, p, x, exps, tops, parts);
+  auto launch = [&](auto zero) {
+    using T = decltype(zero);
+    const XIn<T> x = {static_cast<const T*>(a.x), a.ldx, a.x_scales, a.x_group,
+                      a.x_group ? static_cast<int>((a.m + a.x_group - 1) / a.x_group) : 1};
+    hipLaunchKernelGGL((columns_kernel<J, LO, T>), grid, dim3(64 * p.waves), 0, s, a, p, x, parts);
+  };
+  if (a.x_dtype == KASHIN_E4M3) launch(e4m3_t());
+  else with_float_type(a.x_dtype, launch);
   return hipGetLastError();
 }
 
@@ -1308,7 +1380,6 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   const bool lo = a.y_dtype != KASHIN_BF16;  // as the rows' product
   const ColumnsPlan p = plan_columns(a.n, a.m, a.groups, a.t, a.experts, a.offsets != nullptr, lo);
   const ColumnsWork at = columns_work(p, a.n, a.m, a.groups, a.t, a.experts);
-  float* x = reinterpret_cast<float*>(a.work + at.x);
   int32_t* exps = reinterpret_cast<int32_t*>(a.work + at.exps);
   uint32_t* tops = reinterpret_cast<uint32_t*>(a.work + at.tops);
   float* zv = reinterpret_cast<float*>(a.work + at.zv);
@@ -1316,34 +1387,28 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   float* parts = reinterpret_cast<float*>(a.work + at.parts);
   _Float16* units = reinterpret_cast<_Float16*>(a.work + at.x);
   const int64_t per_expert = a.m * a.groups * 8, slices = static_cast<int64_t>(a.experts) * kTopSlices;
-  auto scale = [&](auto zero) {
-    using T = decltype(zero);
-    const T* rows = static_cast<const T*>(a.x);
-    if (p.tiled)
-      hipLaunchKernelGGL((split_columns_kernel<T>), dim3(static_cast<unsigned>((a.t + kUnitRows - 1) / kUnitRows + slices)),
-                         dim3(kSplitT), 0, s, rows, a.ldx, a.x_scales, a.x_group, a.m, a.t, lo ? 2 : 1, a.centers, per_expert,
-                         units, exps, tops);
-    else
-      hipLaunchKernelGGL((scale_columns_kernel<T>), dim3(static_cast<unsigned>(a.t + slices)), dim3(kScaleT), 0, s, rows, a.ldx,
-                         a.x_scales, a.x_group, a.m, a.t, a.centers, per_expert, x, exps, tops);
-    return hipGetLastError();
-  };
-  hipError_t e = a.x_dtype == KASHIN_E4M3 ? scale(e4m3_t()) : with_float_type(a.x_dtype, scale);
-  if (e != hipSuccess) return e;
+  hipError_t e = hipSuccess;
   if (p.tiled) {
+    auto split = [&](auto zero) {
+      using T = decltype(zero);
+      hipLaunchKernelGGL((split_columns_kernel<T>), dim3(static_cast<unsigned>((a.t + kUnitRows - 1) / kUnitRows + slices)),
+                         dim3(kSplitT), 0, s, static_cast<const T*>(a.x), a.ldx, a.x_scales, a.x_group, a.m, a.t, lo ? 2 : 1,
+                         a.centers, per_expert, units, exps, tops);
+      return hipGetLastError();
+    };
+    e = a.x_dtype == KASHIN_E4M3 ? split(e4m3_t()) : with_float_type(a.x_dtype, split);
+    if (e != hipSuccess) return e;
     const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.per_group) * a.groups * 2 * p.splits),
                     static_cast<unsigned>(p.tiles));
     if (lo) hipLaunchKernelGGL((columns_tile_kernel<true>), grid, dim3(512), 0, s, a, p, units, exps, tops, parts);
     else hipLaunchKernelGGL((columns_tile_kernel<false>), grid, dim3(512), 0, s, a, p, units, exps, tops, parts);
     e = hipGetLastError();
   } else if (lo) {
-    e = p.j == 0   ? launch_columns<0, 16, true>(a, p, x, exps, tops, parts, s)
-        : p.j == 1 ? launch_columns<1, 16, true>(a, p, x, exps, tops, parts, s)
-                   : launch_columns<2, 16, true>(a, p, x, exps, tops, parts, s);
+    e = p.j == 0   ? launch_columns<0, true>(a, p, parts, s)
+        : p.j == 1 ? launch_columns<1, true>(a, p, parts, s)
+                   : launch_columns<2, true>(a, p, parts, s);
   } else {
-    e = p.j == 1   ? launch_columns<1, 16, false>(a, p, x, exps, tops, parts, s)
-        : p.j == 2 ? launch_columns<2, 16, false>(a, p, x, exps, tops, parts, s)
-                   : launch_columns<4, 8, false>(a, p, x, exps, tops, parts, s);
+    e = p.j == 1 ? launch_columns<1, false>(a, p, parts, s) : launch_columns<2, false>(a, p, parts, s);
   }
   if (e != hipSuccess) return e;
   const dim3 whole(static_cast<unsigned>(a.t), static_cast<unsigned>((k + 255) / 256));
