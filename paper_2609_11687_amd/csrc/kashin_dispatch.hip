@@ -36,7 +36,9 @@ namespace kashin {
   X(14336, 512, 2, 32, 14, 32)  \
   X(16384, 512, 2, 32, 16, 32)
 
-#define X(N, ...) hipError_t launch_n##N(const KArgs& a, int64_t grid, hipStream_t stream);
+#define X(N, ...)                                                             \
+  hipError_t launch_n##N(const KArgs& a, int64_t grid, hipStream_t stream);    \
+  hipError_t layer_n##N(const LayerArgs& a, hipStream_t stream);
 KASHIN_SIZES(X)
 #undef X
 
@@ -149,6 +151,18 @@ hipError_t launch_pair(int n, const KArgs& a, int64_t grid, hipStream_t stream) 
 #define X(N, ...) \
   case N:         \
     return launch_n##N(a, grid, stream);
+    KASHIN_SIZES(X)
+#undef X
+    default:
+      return hipErrorInvalidValue;
+  }
+}
+
+hipError_t launch_layer(int n, const LayerArgs& a, hipStream_t stream) {
+  switch (n) {
+#define X(N, ...) \
+  case N:         \
+    return layer_n##N(a, stream);
     KASHIN_SIZES(X)
 #undef X
     default:

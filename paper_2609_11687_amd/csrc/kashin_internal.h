@@ -219,6 +219,20 @@ struct NormArgs {
 constexpr int kNormMaxN = 16384;
 hipError_t launch_rmsnorm(const NormArgs& a, int dtype, hipStream_t stream);
 
+// Rows of x to operands of x and P x (kashin_layer_impl.h; the operands' layout: kashin_units.h).
+struct LayerArgs {
+  const float2* tw;
+  const float4* mid4;
+  int64_t rows;
+  const void* x;
+  int x_dtype;  // KASHIN_F32, _F16 or _BF16
+  int64_t ldx;
+  _Float16* frags;
+  int32_t* exps;
+  int parts;
+};
+hipError_t launch_layer(int n, const LayerArgs& a, hipStream_t stream);
+
 // Products from the codes (kashin_matmul.hip); the fields are kashin_matmul's arguments.
 struct ProductArgs {
   KArgs p;  // the plan's operator tables, for P

@@ -3,6 +3,7 @@
 // grouped by expert.
 #include "kashin_internal.h"
 #include "kashin_rows.h"
+#include "kashin_units.h"
 
 namespace kashin {
 namespace {
@@ -129,48 +130,13 @@ __device__ __forceinline__ void put(void* y, int dtype, int64_t i, float v) {
   else static_cast<__bf16*>(y)[i] = static_cast<__bf16>(v);
 }
 
-template <class T>
-__device__ __forceinline__ void put4_as(T* y, int64_t valid, const float (&v)[4]) {
-  T q[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) q[j] = static_cast<T>(v[j]);
-  if (valid >= 4) {
-    __builtin_memcpy(y, q, sizeof(q));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < valid) y[j] = q[j];
-  }
-}
-// Four entries from i on, of which `valid` exist.
-__device__ __forceinline__ void put4(void* y, int dtype, int64_t i, int64_t valid, const float (&v)[4]) {
-  if (dtype == KASHIN_F32) put4_as(static_cast<float*>(y) + i, valid, v);
-  else if (dtype == KASHIN_F16) put4_as(static_cast<_Float16*>(y) + i, valid, v);
-  else put4_as(static_cast<__bf16*>(y) + i, valid, v);
-}
-
 // ------------------------------------------------------------------ operands of the matrix instructions
 // Products run on fp16 matrix instructions with fp32 sums.  fp32 operands are two fp16 parts, hi + lo, which hold 22
 // bits: x y = hi hi + hi lo + lo hi to 2^-21.  Both operands are scaled by powers of two first, a row of x with P x and a
 // matrix row's centres each by its largest magnitude, into fp16's range.
-using half8 = _Float16 __attribute__((ext_vector_type(8)));
-using float4_t = float __attribute__((ext_vector_type(4)));
 using uint4_t = uint32_t __attribute__((ext_vector_type(4)));
 
-constexpr int kChunk = 64;  // codes a lane decodes from one 16-byte load
-constexpr int kUnits = 8;   // units of 8 codes in a chunk: one operand register block of a matrix instruction each
 constexpr int kRowsT = 512;
-constexpr int kSlab = 4;    // chunks that the four quarters of a wave work on side by side
-
-__host__ __device__ inline int chunks_per_group(int n) { return (n + kChunk - 1) / kChunk; }
-// chunks of a factor, to a multiple of the slab (the last ones may be empty)
-__host__ __device__ inline int64_t padded_chunks(int n, int groups) {
-  return (static_cast<int64_t>(groups) * chunks_per_group(n) + kSlab - 1) / kSlab * kSlab;
-}
-
-// Entry k of a unit's eight: units 2d and 2d + 1 of a chunk come from its dword d, whose 16 codes leave four at a time, two
-// bits of every byte.
-__device__ constexpr int unit_entry(int unit, int k) { return 16 * (unit / 2) + 2 * (unit % 2) + k / 4 + 4 * (k % 4); }
 
 // Exponent s that takes a largest magnitude (as bits) into [2^13, 2^14) when multiplied by 2^s; NaN or infinity: none.
 __device__ __forceinline__ int scale_exponent(uint32_t top) {
@@ -247,9 +213,6 @@ __device__ __forceinline__ uint4_t load_codes(const uint8_t* group, int nby, int
 }
 
 // ------------------------------------------------------------------ x W^T: x and P x as operands
-// frags[factor][unit][part][row][8]: hi (part 0) and, where there are `parts` = 2, lo parts of scaled x (factor 0) and
-// P x, eight entries of a row in the order of a unit's codes; rows innermost, so that the lanes of a matrix instruction's
-// operand read consecutive 16 bytes.  exps[row]: the exponent of the scale.  One workgroup a row.
 // A workgroup takes ROWS rows (8: the lanes of eight rows write 128 consecutive bytes; 1 where there are few
 // rows, to spread them over the chip), a thread 16 entries of a row at a time: two units.
 constexpr int kSplitT = 512;
@@ -314,20 +277,7 @@ __global__ __launch_bounds__(kSplitT) void split_rows_kernel(XRows x, const floa
     float v[16];
     if (b < blocks) load16(0, b, v);
     else load16(1, b - blocks, v);
-    half8 h[2], l[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float w = v[unit_entry(u, j)] * scale;
-        h[u][j] = static_cast<_Float16>(w);
-        l[u][j] = static_cast<_Float16>(w - static_cast<float>(h[u][j]));
-      }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      *reinterpret_cast<half8*>(frags + ((2 * b + u) * parts * t + row) * 8) = h[u];
-      if (parts == 2) *reinterpret_cast<half8*>(frags + ((2 * b + u) * 2 * t + t + row) * 8) = l[u];
-    }
+    put_units(frags, b, parts, t, row, v, scale);
   }
 }
 
@@ -1379,6 +1329,7 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   const int64_t k = static_cast<int64_t>(a.groups) * a.n;
   const bool lo = a.y_dtype != KASHIN_BF16;  // as the rows' product
   const ColumnsPlan p = plan_columns(a.n, a.m, a.groups, a.t, a.experts, a.offsets != nullptr, lo);
+  if (p.splits * a.t > p.part_rows) return hipErrorInvalidValue;  // the bound holds: never
   const ColumnsWork at = columns_work(p, a.n, a.m, a.groups, a.t, a.experts);
   int32_t* exps = reinterpret_cast<int32_t*>(a.work + at.exps);
   uint32_t* tops = reinterpret_cast<uint32_t*>(a.work + at.tops);
@@ -1426,6 +1377,26 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The product itself, by the rows that a matrix meets.
+hipError_t launch_product_rows(const ProductArgs& a, const _Float16* frags, const int32_t* exps, int64_t each, bool lo,
+                               hipStream_t s) {
+  if (each <= 8 && lo) return launch_rows<0, 1, true>(a, frags, exps, s);
+  if (each <= 16) return lo ? launch_rows<1, 1, true>(a, frags, exps, s) : launch_rows<1, 1, false>(a, frags, exps, s);
+  // enough tiles of 256 x 128 to fill the chip
+  if (each >= 96 && ((a.m + kTileM - 1) / kTileM) * (a.t / kTileT) >= 128) {
+    const dim3 grid(static_cast<unsigned>((a.m + kTileM - 1) / kTileM),
+                    static_cast<unsigned>(most_tiles(a.offsets != nullptr, a.t, a.experts, kTileT)));
+    const bool aligned = a.n % (kChunk * kSlab) == 0;
+    if (lo && aligned) hipLaunchKernelGGL((rows_tile_kernel<true, true>), grid, dim3(512), 0, s, a, frags, exps);
+    else if (lo) hipLaunchKernelGGL((rows_tile_kernel<true, false>), grid, dim3(512), 0, s, a, frags, exps);
+    else if (aligned) hipLaunchKernelGGL((rows_tile_kernel<false, true>), grid, dim3(512), 0, s, a, frags, exps);
+    else hipLaunchKernelGGL((rows_tile_kernel<false, false>), grid, dim3(512), 0, s, a, frags, exps);
+    return hipGetLastError();
+  }
+  if (lo) return each <= 32 ? launch_rows<2, 2, true>(a, frags, exps, s) : launch_rows<4, 2, true>(a, frags, exps, s);
+  return each <= 32 ? launch_rows<2, 2, false>(a, frags, exps, s) : launch_rows<4, 2, false>(a, frags, exps, s);
+}
+
 }  // namespace
 
 int64_t product_workspace_bytes(int n, int64_t m, int groups, int64_t t, int experts, bool back) {
@@ -1458,7 +1429,15 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
     e = launch_rotate(a.n, a.rot_seed, false, x.p, x.dtype, a.groups == 1 ? x.ld : a.n, wide, a.n, a.t * a.groups, s);
     x = {wide, k, KASHIN_F32};
   }
-  if (e == hipSuccess) e = apply_p(a, x, px, s);
+  if (e != hipSuccess) return e;
+  // P writes the operands itself where a row's group is the row; for many rows its 32-byte pieces of them cost more than a
+  // pass of their own
+  if (a.groups == 1 && a.t < 64) {
+    const LayerArgs l = {a.p.tw, a.p.mid4, a.t, x.p, x.dtype, x.ld, frags, exps, parts};
+    e = launch_layer(a.n, l, s);
+    return e != hipSuccess ? e : launch_product_rows(a, frags, exps, each, lo, s);
+  }
+  e = apply_p(a, x, px, s);
   if (e != hipSuccess) return e;
 
   if (a.t >= 64)
@@ -1469,21 +1448,7 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
                        parts, frags, exps);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (each <= 8 && lo) return launch_rows<0, 1, true>(a, frags, exps, s);
-  if (each <= 16) return lo ? launch_rows<1, 1, true>(a, frags, exps, s) : launch_rows<1, 1, false>(a, frags, exps, s);
-  // enough tiles of 256 x 128 to fill the chip
-  if (each >= 96 && ((a.m + kTileM - 1) / kTileM) * (a.t / kTileT) >= 128) {
-    const dim3 grid(static_cast<unsigned>((a.m + kTileM - 1) / kTileM),
-                    static_cast<unsigned>(most_tiles(a.offsets != nullptr, a.t, a.experts, kTileT)));
-    const bool aligned = a.n % (kChunk * kSlab) == 0;
-    if (lo && aligned) hipLaunchKernelGGL((rows_tile_kernel<true, true>), grid, dim3(512), 0, s, a, frags, exps);
-    else if (lo) hipLaunchKernelGGL((rows_tile_kernel<true, false>), grid, dim3(512), 0, s, a, frags, exps);
-    else if (aligned) hipLaunchKernelGGL((rows_tile_kernel<false, true>), grid, dim3(512), 0, s, a, frags, exps);
-    else hipLaunchKernelGGL((rows_tile_kernel<false, false>), grid, dim3(512), 0, s, a, frags, exps);
-    return hipGetLastError();
-  }
-  if (lo) return each <= 32 ? launch_rows<2, 2, true>(a, frags, exps, s) : launch_rows<4, 2, true>(a, frags, exps, s);
-  return each <= 32 ? launch_rows<2, 2, false>(a, frags, exps, s) : launch_rows<4, 2, false>(a, frags, exps, s);
+  return launch_product_rows(a, frags, exps, each, lo, s);
 }
 
 }  // namespace kashin

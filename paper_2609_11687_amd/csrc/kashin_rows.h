@@ -69,6 +69,26 @@ __device__ __forceinline__ void store8(e4m3_t* p, int valid, const float (&v)[8]
   }
 }
 
+template <class T>
+__device__ __forceinline__ void put4_as(T* y, int64_t valid, const float (&v)[4]) {
+  T q[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) q[j] = static_cast<T>(v[j]);
+  if (valid >= 4) {
+    __builtin_memcpy(y, q, sizeof(q));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < valid) y[j] = q[j];
+  }
+}
+// Four entries of KASHIN_F32, _F16 or _BF16 rows from i on, of which `valid` exist.
+__device__ __forceinline__ void put4(void* y, int dtype, int64_t i, int64_t valid, const float (&v)[4]) {
+  if (dtype == KASHIN_F32) put4_as(static_cast<float*>(y) + i, valid, v);
+  else if (dtype == KASHIN_F16) put4_as(static_cast<_Float16*>(y) + i, valid, v);
+  else put4_as(static_cast<__bf16*>(y) + i, valid, v);
+}
+
 // f(T()) for the element type of a KASHIN_F32 / _F16 / _BF16 code (checked by the caller)
 template <class F>
 auto with_float_type(int dtype, F&& f) {
