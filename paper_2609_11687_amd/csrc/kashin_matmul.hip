@@ -488,11 +488,11 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
   }
 }
 
-// y = x W^T for many rows of x: a workgroup computes 256 matrix rows by 128 rows of x, wave (rw, cw) 64 by 64 of them in
-// 32 x 32 tiles.  The rows of x pass through LDS (128 entries of K of one factor at a time, two buffers, filled by loads
-// that go to LDS directly); a wave decodes its 64 matrix rows' codes in registers, each code once for 64 rows of x.
+// y = x W^T for many rows of x: a workgroup computes 256 matrix rows by TT rows of x in 32 x 32 tiles: 128 rows of x, wave
+// (rw, cw) 64 by 64 of them, or 64, a wave 32 by 64.  The rows of x pass through LDS (128 entries of K of one factor at a time, two buffers, filled by loads
+// that go to LDS directly); a wave decodes its matrix rows' codes in registers, each code once for 64 rows of x.
 using float16_t = float __attribute__((ext_vector_type(16)));
-constexpr int kTileM = 256, kTileT = 128;
+constexpr int kTileM = 256;
 
 // 16 bytes a lane from memory to LDS, lane by lane behind `lds` (the same in all lanes).  Written as an instruction: the
 // compiler would let every later LDS read wait for it, also of the other buffer.  It has no register output; who reads the
@@ -507,58 +507,59 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-template <bool LO, bool ALIGNED>
+template <int TT, bool LO, bool ALIGNED>
 __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const _Float16* frags, const int32_t* exps) {
   constexpr int PARTS = LO ? 2 : 1, SU = 2 * kUnits;  // units of a slab: two chunks
-  __shared__ __align__(16) _Float16 xs[2][PARTS][SU][kTileT][8];
+  constexpr int RT = TT / 64;                         // tiles of matrix rows of a wave; two of rows of x
+  __shared__ __align__(16) _Float16 xs[2][PARTS][SU][TT][8];
   __shared__ uint32_t tops[kTileM];
-  const Tile tl = find_tile<kTileT>(a.offsets, a.experts, a.t, blockIdx.y);
+  const Tile tl = find_tile<TT>(a.offsets, a.experts, a.t, blockIdx.y);
   if (tl.rows == 0) return;
   const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
-  const int r = lane % 32, q = lane / 32, rw = wave / 2, cw = wave % 2, cpg = chunks_per_group(n), groups = a.groups;
+  const int r = lane % 32, q = lane / 32, rw = wave / RT, cw = wave % RT, cpg = chunks_per_group(n), groups = a.groups;
   const int chunks = groups * cpg;
   const int64_t units = padded_chunks(n, groups) * kUnits;
   const int slabs = (chunks + 1) / 2, items = 2 * slabs, per_group = cpg / 2;  // per_group: ALIGNED
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTileM, matrix0 = (tl.expert * a.m + row0) * groups;
-  uint32_t crow[2];  // this lane's matrix rows (past the last repeat it), as offsets from the workgroup's first
+  uint32_t crow[RT];  // this lane's matrix rows (past the last repeat it), as offsets from the workgroup's first
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < RT; ++i) {
     const int64_t left = a.m - 1 - row0;
-    const int at = 64 * rw + 32 * i + r;
+    const int at = 32 * (RT * rw + i) + r;
     crow[i] = static_cast<uint32_t>((at < left ? at : left) * groups);
   }
   const uint8_t* cu = a.codes_u + matrix0 * nby;
   const uint8_t* cv = a.codes_v + matrix0 * nby;
   const float* ce = a.centers + matrix0 * 8;
-  auto load_item = [&](int it, uint4_t (&c)[2]) {
+  auto load_item = [&](int it, uint4_t (&c)[RT]) {
     const int f = it >= slabs, slab = it - f * slabs;
     const uint8_t* base = f ? cv : cu;
     if constexpr (ALIGNED) {
       base += slab * 32;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < RT; ++i)
         __builtin_memcpy(&c[i], base + static_cast<uint32_t>(crow[i] * static_cast<uint32_t>(nby) + 16 * q), 16);
     } else {
       const int chunk = slab * 2 + q, at = chunk < chunks ? chunk : chunks - 1, g = at / cpg;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < RT; ++i)
         c[i] = load_codes(base + static_cast<uint32_t>((crow[i] + g) * static_cast<uint32_t>(nby)), nby, (at - g * cpg) * 16);
     }
   };
-  auto fill = [&](int it, int buf) {
-    const int f = it >= slabs, c = (wave % 2) * 64 + lane;
+  auto fill = [&](int it, int buf) {  // a wave's load takes 64 rows of x of a unit
+    const int f = it >= slabs, c = (wave % RT) * 64 + lane;
     const int64_t u0 = f * units + static_cast<int64_t>(it - f * slabs) * SU;
     const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
 #pragma unroll
     for (int pt = 0; pt < PARTS; ++pt)
 #pragma unroll
-      for (int k = 0; k < SU / 4; ++k) {
-        const int u = 4 * k + wave / 2;
-        load_to_lds(frags + (((u0 + u) * PARTS + pt) * a.t + row) * 8, &xs[buf][pt][u][(wave % 2) * 64][0]);
+      for (int k = 0; k < SU * RT / 8; ++k) {
+        const int u = 8 / RT * k + wave / RT;
+        load_to_lds(frags + (((u0 + u) * PARTS + pt) * a.t + row) * 8, &xs[buf][pt][u][(wave % RT) * 64][0]);
       }
   };
   // codes are loaded two items ahead: an item takes less time than memory does
-  uint4_t next[2][2];
+  uint4_t next[2][RT];
   load_item(0, next[0]);
   fill(0, 0);
   load_item(1, next[1]);  // items is even
@@ -581,20 +582,20 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
   }
   wait_loads<0>();
   __syncthreads();
-  float scale[2];
+  float scale[RT];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t top = tops[64 * rw + 32 * i + r];
+  for (int i = 0; i < RT; ++i) {
+    const uint32_t top = tops[32 * (RT * rw + i) + r];
     scale[i] = top >= kInfBits ? __int_as_float(0x7fc00000) : power_of_two(scale_exponent(top));
   }
-  float16_t acc[2][2];
+  float16_t acc[RT][2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
-  Table tb[2];
+  Table tb[RT];
   int held = -1;
   for (int b0 = 0; b0 < items; b0 += 2) {
 #pragma unroll
@@ -607,30 +608,33 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
         const int chunk = slab * 2 + q;
         g = (chunk < chunks ? chunk : chunks - 1) / cpg;
       }
-      uint4_t now[2] = {next[buf][0], next[buf][1]};
+      uint4_t now[RT];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) now[i] = next[buf][i];
       // taken before the loads to LDS are issued: the compiler counts its own loads only, and would wait for those too
-      asm volatile("" : "+v"(now[0]), "+v"(now[1]));
+#pragma unroll
+      for (int i = 0; i < RT; ++i) asm volatile("" : "+v"(now[i]));
       fill(it + 1 < items ? it + 1 : it, buf ^ 1);  // past the last item: what nobody reads
       if (f * groups + g != held) {
         held = f * groups + g;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < RT; ++i)
           tb[i] = make_table(*reinterpret_cast<const float4_t*>(ce + 8 * g + 4 * f + static_cast<uint32_t>(crow[i] * 8)), scale[i]);
       }
       load_item(it + 2 < items ? it + 2 : items - 1, next[buf]);
       __builtin_amdgcn_sched_barrier(0);  // issued here, not behind the products
 #pragma unroll
       for (int s = 0; s < kUnits; ++s) {
-        half8 hi[2], lo[2], xh[2], xl[2];
+        half8 hi[RT], lo[RT], xh[2], xl[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           xh[j] = *reinterpret_cast<const half8*>(&xs[buf][0][q * kUnits + s][64 * cw + 32 * j + r][0]);
           if constexpr (LO) xl[j] = *reinterpret_cast<const half8*>(&xs[buf][1][q * kUnits + s][64 * cw + 32 * j + r][0]);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) decode8<LO>(now[i][s / 2], s % 2, tb[i], hi[i], lo[i]);
+        for (int i = 0; i < RT; ++i) decode8<LO>(now[i][s / 2], s % 2, tb[i], hi[i], lo[i]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             if constexpr (LO) {
@@ -640,8 +644,8 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi[i], xh[j], acc[i][j], 0, 0, 0);
           }
       }
-      // x of the next item has arrived when at most the two loads of codes behind it are under way
-      wait_loads<ALIGNED ? 2 : 0>();
+      // x of the next item has arrived when at most the loads of codes behind it are under way
+      wait_loads<ALIGNED ? RT : 0>();
       __syncthreads();
     }
   }
@@ -651,10 +655,10 @@ __global__ __launch_bounds__(512, 2) void rows_tile_kernel(ProductArgs a, const 
     if (c >= tl.rows) continue;
     const int ex = exps[tl.row0 + c];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        const int in_tile = 64 * rw + 32 * i + 8 * b + 4 * q;
+        const int in_tile = 32 * (RT * rw + i) + 8 * b + 4 * q;
         float v[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -1254,6 +1258,17 @@ hipError_t launch_rows(const ProductArgs& a, const _Float16* frags, const int32_
   return hipGetLastError();
 }
 
+template <int TT, bool LO>
+hipError_t launch_rows_tile(const ProductArgs& a, const _Float16* frags, const int32_t* exps, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>((a.m + kTileM - 1) / kTileM),
+                  static_cast<unsigned>(most_tiles(a.offsets != nullptr, a.t, a.experts, TT)));
+  if (a.n % (kChunk * kSlab) == 0)
+    hipLaunchKernelGGL((rows_tile_kernel<TT, LO, true>), grid, dim3(512), 0, s, a, frags, exps);
+  else
+    hipLaunchKernelGGL((rows_tile_kernel<TT, LO, false>), grid, dim3(512), 0, s, a, frags, exps);
+  return hipGetLastError();
+}
+
 // Rows of x that a matrix (an expert's, on average) meets.
 int64_t rows_each(int64_t t, int experts) { return t / (experts < t ? experts : t > 0 ? t : 1); }
 
@@ -1382,17 +1397,12 @@ hipError_t launch_product_rows(const ProductArgs& a, const _Float16* frags, cons
                                hipStream_t s) {
   if (each <= 8 && lo) return launch_rows<0, 1, true>(a, frags, exps, s);
   if (each <= 16) return lo ? launch_rows<1, 1, true>(a, frags, exps, s) : launch_rows<1, 1, false>(a, frags, exps, s);
-  // enough tiles of 256 x 128 to fill the chip
-  if (each >= 96 && ((a.m + kTileM - 1) / kTileM) * (a.t / kTileT) >= 128) {
-    const dim3 grid(static_cast<unsigned>((a.m + kTileM - 1) / kTileM),
-                    static_cast<unsigned>(most_tiles(a.offsets != nullptr, a.t, a.experts, kTileT)));
-    const bool aligned = a.n % (kChunk * kSlab) == 0;
-    if (lo && aligned) hipLaunchKernelGGL((rows_tile_kernel<true, true>), grid, dim3(512), 0, s, a, frags, exps);
-    else if (lo) hipLaunchKernelGGL((rows_tile_kernel<true, false>), grid, dim3(512), 0, s, a, frags, exps);
-    else if (aligned) hipLaunchKernelGGL((rows_tile_kernel<false, true>), grid, dim3(512), 0, s, a, frags, exps);
-    else hipLaunchKernelGGL((rows_tile_kernel<false, false>), grid, dim3(512), 0, s, a, frags, exps);
-    return hipGetLastError();
-  }
+  // enough tiles of 256 x 128, or 256 x 64, to fill half the chip
+  const int64_t row_tiles = (a.m + kTileM - 1) / kTileM;
+  if (each >= 96 && row_tiles * (a.t / 128) >= 128)
+    return lo ? launch_rows_tile<128, true>(a, frags, exps, s) : launch_rows_tile<128, false>(a, frags, exps, s);
+  if (each > 32 && row_tiles * (a.t / 64) >= 128)
+    return lo ? launch_rows_tile<64, true>(a, frags, exps, s) : launch_rows_tile<64, false>(a, frags, exps, s);
   if (lo) return each <= 32 ? launch_rows<2, 2, true>(a, frags, exps, s) : launch_rows<4, 2, true>(a, frags, exps, s);
   return each <= 32 ? launch_rows<2, 2, false>(a, frags, exps, s) : launch_rows<4, 2, false>(a, frags, exps, s);
 }

@@ -275,7 +275,8 @@ def test_products_of_groups_and_rotations(n, groups, m, rot, back):
 
 
 @pytest.mark.parametrize("back", [False, True])
-@pytest.mark.parametrize("n,groups,m,t", [(256, 2, 4100, 1050), (64, 1, 33000, 200), (96, 3, 8200, 511), (512, 1, 2100, 2049)])
+@pytest.mark.parametrize("n,groups,m,t", [(256, 2, 4100, 1050), (64, 1, 33000, 200), (96, 3, 8200, 511), (512, 1, 2100, 2049), (256, 2, 11000, 195),
+                                          (172, 1, 9000, 250)])
 def test_products_of_many_rows(n, groups, m, t, back):
     print(f"product n={n} groups={groups} m={m} t={t} back={back}", flush=True)
     case = Case(n, m, groups)
