@@ -38,7 +38,8 @@ namespace kashin {
 
 #define X(N, ...)                                                             \
   hipError_t launch_n##N(const KArgs& a, int64_t grid, hipStream_t stream);    \
-  hipError_t layer_n##N(const LayerArgs& a, hipStream_t stream);
+  hipError_t layer_n##N(const LayerArgs& a, hipStream_t stream);              \
+  hipError_t layer_back_n##N(const LayerBackArgs& a, hipStream_t stream);
 KASHIN_SIZES(X)
 #undef X
 
@@ -163,6 +164,18 @@ hipError_t launch_layer(int n, const LayerArgs& a, hipStream_t stream) {
 #define X(N, ...) \
   case N:         \
     return layer_n##N(a, stream);
+    KASHIN_SIZES(X)
+#undef X
+    default:
+      return hipErrorInvalidValue;
+  }
+}
+
+hipError_t launch_layer_back(int n, const LayerBackArgs& a, hipStream_t stream) {
+  switch (n) {
+#define X(N, ...) \
+  case N:         \
+    return layer_back_n##N(a, stream);
     KASHIN_SIZES(X)
 #undef X
     default:

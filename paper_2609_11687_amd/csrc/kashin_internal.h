@@ -224,14 +224,33 @@ struct LayerArgs {
   const float2* tw;
   const float4* mid4;
   int64_t rows;
+  int groups;  // vectors of a row, behind each other
   const void* x;
-  int x_dtype;  // KASHIN_F32, _F16 or _BF16
+  int x_dtype;
   int64_t ldx;
+  const float* x_scales;
+  int x_group;
   _Float16* frags;
   int32_t* exps;
   int parts;
 };
 hipError_t launch_layer(int n, const LayerArgs& a, hipStream_t stream);
+
+// y = zu + P zv for t rows of `groups` vectors; rows outside the offsets' range keep what they hold.
+struct LayerBackArgs {
+  const float2* tw;
+  const float4* mid4;
+  int64_t t;
+  int groups;
+  const float* zu;
+  const float* zv;
+  const int64_t* offsets;
+  int experts;
+  void* y;
+  int y_dtype;
+  int64_t ldy;
+};
+hipError_t launch_layer_back(int n, const LayerBackArgs& a, hipStream_t stream);
 
 // Products from the codes (kashin_matmul.hip); the fields are kashin_matmul's arguments.
 struct ProductArgs {

@@ -1184,33 +1184,16 @@ __device__ __forceinline__ float4_t sum_parts(const float* p, int64_t stride, in
   return lds[0][at] + lds[1][at] + lds[2][at] + lds[3][at];
 }
 
-// zv = the sum of its parts; zeros for rows that no expert has (P takes rows in pairs, and what lies in a row's
-// neighbour may show in its last bits).  256 columns a workgroup.
-__global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int splits, const float* parts, int64_t k, float* zv) {
+// zu and zv, each the sum of its parts (z: zu of all rows, then zv); zeros for rows that no expert has (P takes rows in
+// pairs, and what lies in a row's neighbour may show in its last bits).  256 columns of one of them a workgroup.
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs a, int splits, const float* parts, int64_t k, float* z) {
   __shared__ float4_t lds[4][64];
   const int at = threadIdx.x % 64, sub = threadIdx.x / 64;
   const int64_t row = blockIdx.x, i = (static_cast<int64_t>(blockIdx.y) * 64 + at) * 4;
   const bool has = covered(a.offsets, a.experts, row) && i < k;
-  const float4_t v = sum_parts(parts + (a.t + row) * k + (has ? i : 0), 2 * a.t * k, has ? splits : 0, sub, lds, at);
-  if (sub == 0 && i < k) *reinterpret_cast<float4_t*>(zv + row * k + i) = v;
-}
-
-// y = zu + P zv, zu the sum of its parts: into y, or as fp32 rows into z (the rotation follows).
-__global__ __launch_bounds__(256) void finish_kernel(ProductArgs a, int splits, const float* parts, const float* pz, int64_t k,
-                                                     float* z) {
-  __shared__ float4_t lds[4][64];
-  const int at = threadIdx.x % 64, sub = threadIdx.x / 64;
-  const int64_t row = blockIdx.x, i = (static_cast<int64_t>(blockIdx.y) * 64 + at) * 4;
-  const bool has = covered(a.offsets, a.experts, row) && i < k;
-  float4_t v = sum_parts(parts + row * k + (has ? i : 0), 2 * a.t * k, has ? splits : 0, sub, lds, at);
-  if (sub != 0 || i >= k || (!has && z == nullptr)) return;
-  if (has) v += *reinterpret_cast<const float4_t*>(pz + row * k + i);
-  if (z != nullptr) {
-    *reinterpret_cast<float4_t*>(z + row * k + i) = v;
-  } else {
-    const float o[4] = {v[0], v[1], v[2], v[3]};
-    put4(a.y, a.y_dtype, row * a.ldy + i, 4, o);
-  }
+  const int64_t mine = (blockIdx.z * a.t + row) * k + (i < k ? i : 0);
+  const float4_t v = sum_parts(parts + mine, 2 * a.t * k, has ? splits : 0, sub, lds, at);
+  if (sub == 0 && i < k) *reinterpret_cast<float4_t*>(z + mine) = v;
 }
 
 // y = z in y's type, covered rows only.
@@ -1312,7 +1295,7 @@ ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, b
 }
 
 struct ColumnsWork {
-  int64_t x, exps, tops, zv, pz, parts, end;
+  int64_t x, exps, tops, z, rz, parts, end;
 };
 ColumnsWork columns_work(const ColumnsPlan& p, int n, int64_t m, int groups, int64_t t, int experts) {
   const int64_t k = static_cast<int64_t>(groups) * n;
@@ -1320,9 +1303,9 @@ ColumnsWork columns_work(const ColumnsPlan& p, int n, int64_t m, int groups, int
   w.x = 0;
   w.exps = w.x + align256(t * column_units(m) * 32);  // units in two parts
   w.tops = w.exps + align256(t * 4);
-  w.zv = w.tops + align256(static_cast<int64_t>(experts) * kTopSlices * 4);
-  w.pz = w.zv + align256(t * k * 4);
-  w.parts = w.pz + align256(t * k * 4);
+  w.z = w.tops + align256(static_cast<int64_t>(experts) * kTopSlices * 4);
+  w.rz = w.z + align256(2 * t * k * 4);
+  w.parts = w.rz + align256(t * k * 4);
   w.end = w.parts + p.part_rows * 2 * k * 4;
   return w;
 }
@@ -1350,8 +1333,8 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   const ColumnsWork at = columns_work(p, a.n, a.m, a.groups, a.t, a.experts);
   int32_t* exps = reinterpret_cast<int32_t*>(a.work + at.exps);
   uint32_t* tops = reinterpret_cast<uint32_t*>(a.work + at.tops);
-  float* zv = reinterpret_cast<float*>(a.work + at.zv);
-  float* pz = reinterpret_cast<float*>(a.work + at.pz);
+  float* z = reinterpret_cast<float*>(a.work + at.z);
+  float* rz = reinterpret_cast<float*>(a.work + at.rz);
   float* parts = reinterpret_cast<float*>(a.work + at.parts);
   _Float16* units = reinterpret_cast<_Float16*>(a.work + at.x);
   const int64_t per_expert = a.m * a.groups * 8, slices = static_cast<int64_t>(a.experts) * kTopSlices;
@@ -1379,18 +1362,26 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
     e = p.j == 1 ? launch_columns<1, false>(a, p, parts, s) : launch_columns<2, false>(a, p, parts, s);
   }
   if (e != hipSuccess) return e;
-  const dim3 whole(static_cast<unsigned>(a.t), static_cast<unsigned>((k + 255) / 256));
-  hipLaunchKernelGGL(join_kernel, whole, dim3(256), 0, s, a, p.splits, parts, k, zv);
-  e = hipGetLastError();
-  if (e == hipSuccess) e = apply_p(a, {zv, k, KASHIN_F32}, pz, s);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(finish_kernel, whole, dim3(256), 0, s, a, p.splits, parts, pz, k, a.rot ? zv : nullptr);
-  e = hipGetLastError();
+  const unsigned rows = static_cast<unsigned>(a.t), strips = static_cast<unsigned>((k + 255) / 256);
+  const float* sums = parts;  // one part of each is its sum
+  if (p.splits > 1 || a.offsets != nullptr) {
+    hipLaunchKernelGGL(join_kernel, dim3(rows, strips, 2), dim3(256), 0, s, a, p.splits, parts, k, z);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    sums = z;
+  }
+  LayerBackArgs back = {a.p.tw, a.p.mid4, a.t, a.groups, sums, sums + a.t * k, a.offsets, a.experts, a.y, a.y_dtype, a.ldy};
+  if (a.rot) {  // fp32 rows of all, which R^T follows
+    back.offsets = nullptr;
+    back.y = rz;
+    back.y_dtype = KASHIN_F32;
+    back.ldy = k;
+  }
+  e = launch_layer_back(a.n, back, s);
   if (e != hipSuccess || !a.rot) return e;
-  e = rotate(a, true, zv, s);
+  e = rotate(a, true, rz, s);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(narrow_kernel, dim3(static_cast<unsigned>(a.t), static_cast<unsigned>((k + 255) / 256)), dim3(256), 0, s,
-                     a, zv, k);
+  hipLaunchKernelGGL(narrow_kernel, dim3(rows, strips), dim3(256), 0, s, a, rz, k);
   return hipGetLastError();
 }
 
@@ -1429,10 +1420,13 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
   const int64_t each = rows_each(a.t, a.experts);
   const bool lo = a.y_dtype != KASHIN_BF16;
   const int parts = lo ? 2 : 1;
-  // the caller's rows where P can read them, else fp32 ones
+  // Up to 63 rows P writes the operands itself; for many rows its 32-byte pieces of them cost more than a pass of their own.
+  // Where a row has several groups, each pair of them looks for the row's largest entry, at most 2^23 entries in all.
+  const bool direct = a.t < 64 && (a.groups == 1 || a.t * a.groups * k <= int64_t(1) << 23);
+  // the caller's rows where the next kernel can read them, else fp32 ones
   XRows x = {a.x, a.ldx, a.x_dtype};
   hipError_t e = hipSuccess;
-  if (a.x_dtype == KASHIN_E4M3 || (a.groups > 1 && a.ldx != k)) {
+  if ((a.rot || !direct) && (a.x_dtype == KASHIN_E4M3 || (a.groups > 1 && a.ldx != k))) {
     e = widen(a, k, wide, s);
     x = {wide, k, KASHIN_F32};
   }
@@ -1442,10 +1436,8 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
     x = {wide, k, KASHIN_F32};
   }
   if (e != hipSuccess) return e;
-  // P writes the operands itself where a row's group is the row; for many rows its 32-byte pieces of them cost more than a
-  // pass of their own
-  if (a.groups == 1 && a.t < 64) {
-    const LayerArgs l = {a.p.tw, a.p.mid4, a.t, x.p, x.dtype, x.ld, frags, exps, parts};
+  if (direct) {
+    const LayerArgs l = {a.p.tw, a.p.mid4, a.t, a.groups, x.p, x.dtype, x.ld, a.x_scales, a.x_group, frags, exps, parts};
     e = launch_layer(a.n, l, s);
     return e != hipSuccess ? e : launch_product_rows(a, frags, exps, each, lo, s);
   }

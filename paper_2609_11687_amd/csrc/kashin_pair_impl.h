@@ -2363,13 +2363,16 @@ hipError_t launch_cfg(const KArgs& a, int64_t grid, hipStream_t s) {
 
 namespace kashin {
 
-// Defines the external launchers launch_n<N> and layer_n<N> for one launch configuration.
+// Defines the external launchers launch_n<N>, layer_n<N> and layer_back_n<N> for one launch configuration.
 #define KASHIN_DEFINE_SIZE(N, T, W, ...)                                                     \
   hipError_t launch_n##N(const KArgs& a, int64_t grid, hipStream_t stream) {                \
     return launch_cfg<Cfg<N, T, W, __VA_ARGS__>>(a, grid, stream);                          \
   }                                                                                          \
   hipError_t layer_n##N(const LayerArgs& a, hipStream_t stream) {                            \
     return launch_layer_cfg<Cfg<N, T, W, __VA_ARGS__>>(a, stream);                           \
+  }                                                                                          \
+  hipError_t layer_back_n##N(const LayerBackArgs& a, hipStream_t stream) {                   \
+    return launch_layer_back_cfg<Cfg<N, T, W, __VA_ARGS__>>(a, stream);                      \
   }
 
 }  // namespace kashin
