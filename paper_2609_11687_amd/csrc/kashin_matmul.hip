@@ -213,9 +213,11 @@ __device__ __forceinline__ uint4_t load_codes(const uint8_t* group, int nby, int
 }
 
 // ------------------------------------------------------------------ x W^T: x and P x as operands
-// A workgroup takes ROWS rows (8: the lanes of eight rows write 128 consecutive bytes; 1 where there are few
-// rows, to spread them over the chip), a thread 16 entries of a row at a time: two units.
+// A workgroup takes ROWS rows (8: the lanes of eight rows write 128 consecutive bytes; 2 below kManyRows, to spread them
+// over the chip: the product of 4096 x 4096 with 128 rows of x 45.7 -> 35.4 us, 1024 rows 151 -> 145, 2000 rows 195.6 ->
+// 197.2), a thread 16 entries of a row at a time: two units.
 constexpr int kSplitT = 512;
+constexpr int kManyRows = 1536;
 template <int ROWS>
 __global__ __launch_bounds__(kSplitT) void split_rows_kernel(XRows x, const float* px, int n, int groups, int64_t t, int parts,
                                                              _Float16* frags, int32_t* exps) {
@@ -256,14 +258,10 @@ __global__ __launch_bounds__(kSplitT) void split_rows_kernel(XRows x, const floa
       top = o > top ? o : top;
     }
   }
-  if constexpr (ROWS == 1) {
-    top = wave_max(top);
-  } else {
 #pragma unroll
-    for (int d = ROWS; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_xor(top, d);
-      top = o > top ? o : top;
-    }
+  for (int d = ROWS; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_xor(top, d);
+    top = o > top ? o : top;
   }
   if (tid % 64 < ROWS) atomicMax(&tops[mine], top);  // a maximum: the same in any order
   __syncthreads();
@@ -705,7 +703,7 @@ __device__ __forceinline__ float load1(const XIn<T>& x, int64_t at, int64_t row,
 // The split of a transposed product: a workgroup of `waves` waves takes as many blocks of columns of one group, over
 // `rows` matrix rows (a multiple of 32), of which there are `splits` per matrix; their sums are joined afterwards.
 struct ColumnsPlan {
-  bool tiled;  // columns_tile_kernel: a workgroup takes 256 columns of a group
+  int tile;  // columns_tile_kernel's rows of x (a workgroup takes 256 columns of a group), or 0
   int j, waves, per_group, splits;
   int64_t rows, tiles, part_rows;
 };
@@ -935,26 +933,27 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
   }
 }
 
-// y = x W for many rows of x: a workgroup computes 128 rows of x by 256 columns of a factor over a range of matrix rows,
-// wave (cw, tw) 64 by 64 of them in 32 x 32 tiles, 32 matrix rows at a time.  The workgroup decodes the 32 x 256 codes once,
+// y = x W for many rows of x: a workgroup computes TT rows of x (128 or 64) by 256 columns of a factor over a range of
+// matrix rows, wave (cw, tw) TT / 2 by 64 of them in 32 x 32 tiles, 32 matrix rows at a time.  The workgroup decodes the 32 x 256 codes once,
 // a dword a thread, into LDS as fp16 rows; operand B takes them with loads that transpose (a lane wants one column of
 // eight matrix rows).  A dword's codes lie in LDS in the order they come out of the tables, 0 4 8 12 1 5 9 13 ..: column
 // 16 d + p / 4 + 4 (p % 4) at place p, which the stores undo.
 // x comes as units of eight matrix rows: units[part][unit][row of x][8], scaled as for x W^T.
-constexpr int kColsM = 32, kColsN = 256, kColsT = 128, kColsLd = kColsN + 32;  // 576-byte rows: four of them on 64 banks
+constexpr int kColsM = 32, kColsN = 256, kColsLd = kColsN + 32;  // 576-byte rows: four of them on 64 banks
 using short4_t = short __attribute__((ext_vector_type(4)));
 
 __host__ __device__ inline int64_t column_units(int64_t m) { return (m + kColsM - 1) / kColsM * (kColsM / 8); }
 
-constexpr int kUnitRows = 8;
-template <class T>
+// x as such units: a workgroup takes ROWS rows (as split_rows_kernel), and behind those workgroups kTopSlices look
+// through an expert's centres each.
+template <int ROWS, class T>
 __global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int64_t ldx, const float* scales, int group, int64_t m,
                                                                 int64_t t, int parts, const float* centers, int64_t per_expert,
                                                                 _Float16* units, int32_t* exps, uint32_t* tops) {
-  __shared__ uint32_t top_of[kUnitRows];
-  const int tid = threadIdx.x, mine = tid % kUnitRows;
-  const int64_t row_blocks = (t + kUnitRows - 1) / kUnitRows;
-  if (tid < kUnitRows) top_of[tid] = 0;
+  __shared__ uint32_t top_of[ROWS];
+  const int tid = threadIdx.x, mine = tid % ROWS;
+  const int64_t row_blocks = (t + ROWS - 1) / ROWS;
+  if (tid < ROWS) top_of[tid] = 0;
   __syncthreads();
   uint32_t top = 0;
   if (blockIdx.x >= row_blocks) {  // the largest finite centre of a slice of an expert's
@@ -974,7 +973,7 @@ __global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int6
     if (tid == 0) tops[id] = top_of[0];
     return;
   }
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kUnitRows + mine;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + mine;
   const bool real = row < t;
   auto load_unit = [&](int64_t u, float (&v)[8]) {
     const int64_t i = 8 * u, left = m - i;
@@ -986,7 +985,7 @@ __global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int6
     }
   };
   const int64_t all = column_units(m);
-  for (int64_t u = tid / kUnitRows; u < all; u += kSplitT / kUnitRows) {
+  for (int64_t u = tid / ROWS; u < all; u += kSplitT / ROWS) {
     float v[8];
     load_unit(u, v);
 #pragma unroll
@@ -1002,8 +1001,8 @@ __global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int6
   const int e = bad ? 0 : scale_exponent(top);
   const float scale = bad ? __int_as_float(0x7fc00000) : power_of_two(e);
   if (!real) return;
-  if (tid < kUnitRows) exps[row] = e;
-  for (int64_t u = tid / kUnitRows; u < all; u += kSplitT / kUnitRows) {
+  if (tid < ROWS) exps[row] = e;
+  for (int64_t u = tid / ROWS; u < all; u += kSplitT / ROWS) {
     float v[8];
     load_unit(u, v);
     half8 h, l;
@@ -1018,14 +1017,14 @@ __global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int6
   }
 }
 
-template <bool LO>
+template <int TT, bool LO>
 __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, ColumnsPlan pl, const _Float16* units,
                                                               const int32_t* exps, const uint32_t* tops, float* out) {
-  constexpr int PARTS = LO ? 2 : 1;
+  constexpr int PARTS = LO ? 2 : 1, I = TT / 64;
   __shared__ __align__(16) _Float16 ws[2][PARTS][kColsM][kColsLd];
-  __shared__ __align__(16) _Float16 xs[2][PARTS][kColsM / 8][kColsT][8];
-  __shared__ int32_t ex[kColsT];
-  const Tile tl = find_tile<kColsT>(a.offsets, a.experts, a.t, blockIdx.y);
+  __shared__ __align__(16) _Float16 xs[2][PARTS][kColsM / 8][TT][8];
+  __shared__ int32_t ex[TT];
+  const Tile tl = find_tile<TT>(a.offsets, a.experts, a.t, blockIdx.y);
   if (tl.rows == 0) return;
   const int n = a.n, nby = n / 4, tid = threadIdx.x, lane = tid % 64, wave = uniform(tid / 64);
   const int r = lane % 32, q = lane / 32, cw = wave / 2, tw = wave % 2;
@@ -1044,7 +1043,7 @@ __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, Col
   }
   const int ec = scale_exponent(top);
   const float cscale = power_of_two(ec);
-  if (tid < kColsT) ex[tid] = tid < tl.rows ? exps[tl.row0 + tid] : 0;
+  if (tid < TT) ex[tid] = tid < tl.rows ? exps[tl.row0 + tid] : 0;
   // this thread's dword of codes: matrix row `mine` of a step, columns 16 d ..; past a group's last byte its last four
   // are read and moved down
   const int mine = tid / 16, d = tid % 16;
@@ -1077,15 +1076,18 @@ __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, Col
   };
   const int64_t all = column_units(a.m);
   auto fill = [&](int64_t k0, int buf) {
-    const int c = (wave % 2) * 64 + lane, u = wave / 2;
-    const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
+    constexpr int PIECES = PARTS * (kColsM / 8) * I;  // of 64 rows: a wave's load
 #pragma unroll
-    for (int pt = 0; pt < PARTS; ++pt)
-      load_to_lds(units + ((pt * all + k0 / 8 + u) * a.t + row) * 8, &xs[buf][pt][u][(wave % 2) * 64][0]);
+    for (int p0 = 0; p0 < PIECES; p0 += 8) {
+      const int p = p0 + wave, h = p % I, u = p / I % (kColsM / 8), pt = p / I / (kColsM / 8), c = 64 * h + lane;
+      if (PIECES < 8 && p >= PIECES) break;
+      const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
+      load_to_lds(units + ((pt * all + k0 / 8 + u) * a.t + row) * 8, &xs[buf][pt][u][64 * h][0]);
+    }
   };
-  float16_t acc[2][2];
+  float16_t acc[I][2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < I; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -1115,12 +1117,12 @@ __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, Col
     __builtin_amdgcn_sched_barrier(0);  // issued here, not behind the products
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
-      half8 x[2][PARTS], b[2][PARTS];
+      half8 x[I][PARTS], b[2][PARTS];
 #pragma unroll
       for (int pt = 0; pt < PARTS; ++pt) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          x[i][pt] = *reinterpret_cast<const half8*>(&xs[buf][pt][2 * ks + q][64 * tw + 32 * i + r][0]);
+        for (int i = 0; i < I; ++i)
+          x[i][pt] = *reinterpret_cast<const half8*>(&xs[buf][pt][2 * ks + q][32 * (I * tw + i) + r][0]);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           union {
@@ -1135,7 +1137,7 @@ __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, Col
         }
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           if constexpr (LO) {
@@ -1153,10 +1155,10 @@ __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, Col
   }
   const int64_t k = static_cast<int64_t>(a.groups) * n;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < I; ++i)
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      const int c = 64 * tw + 32 * i + 8 * (v / 4) + 4 * q + v % 4;
+      const int c = 32 * (I * tw + i) + 8 * (v / 4) + 4 * q + v % 4;
       if (c >= tl.rows) continue;
       float* o = out + ((static_cast<int64_t>(split) * 2 + f) * a.t + tl.row0 + c) * k + static_cast<int64_t>(g) * n;
 #pragma unroll
@@ -1277,12 +1279,16 @@ ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, b
   // tiles of at most 32 rows each want their share of `fill`
   const int64_t bound = (fill / one + 1) * 32 + t;
   p.part_rows = most * t < bound ? most * t : bound;
-  p.tiled = each >= 48;
-  if (p.tiled) {
+  // From 48 rows of x a matrix on, tiles.  Of 64 rows where 128 would be half empty; where experts' rows end in a tile's
+  // middle 64 also pay up to 128 rows a matrix with hi and lo parts, whose products hide the codes' decoding (8 experts, 2048 x
+  // 4096, fp32 results, us with 64 and 128: 400 rows 131 and 152, 700 rows 156 and 191, 1500 rows 288 and 248; bf16: 400
+  // rows 81 and 84, 700 rows 96 and 92).
+  p.tile = each < 48 ? 0 : (grouped ? each < (lo ? 128 : 64) : t <= 64) ? 64 : 128;
+  if (p.tile) {
     p.per_group = (n + kColsN - 1) / kColsN;
-    p.tiles = most_tiles(grouped, t, experts, kColsT);
+    p.tiles = most_tiles(grouped, t, experts, p.tile);
     // two workgroups a compute unit, of at least 256 matrix rows each; never more than the bound above, whose tiles
-    // are a quarter of these and whose workgroups take 2048 columns
+    // are half of these or less and whose workgroups take 2048 columns
     const int64_t others = static_cast<int64_t>(p.per_group) * groups * 2 * p.tiles;
     const int64_t wanted = (512 + others - 1) / others, top = (m + 255) / 256, cut = wanted < top ? wanted : top;
     p.rows = ((m + cut - 1) / cut + 31) / 32 * 32;
@@ -1325,6 +1331,15 @@ hipError_t launch_columns(const ProductArgs& a, const ColumnsPlan& p, float* par
   return hipGetLastError();
 }
 
+template <int TT, bool LO>
+hipError_t launch_columns_tile(const ProductArgs& a, const ColumnsPlan& p, const _Float16* units, const int32_t* exps,
+                               const uint32_t* tops, float* parts, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.per_group) * a.groups * 2 * p.splits),
+                  static_cast<unsigned>(p.tiles));
+  hipLaunchKernelGGL((columns_tile_kernel<TT, LO>), grid, dim3(512), 0, s, a, p, units, exps, tops, parts);
+  return hipGetLastError();
+}
+
 hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   const int64_t k = static_cast<int64_t>(a.groups) * a.n;
   const bool lo = a.y_dtype != KASHIN_BF16;  // as the rows' product
@@ -1339,21 +1354,25 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   _Float16* units = reinterpret_cast<_Float16*>(a.work + at.x);
   const int64_t per_expert = a.m * a.groups * 8, slices = static_cast<int64_t>(a.experts) * kTopSlices;
   hipError_t e = hipSuccess;
-  if (p.tiled) {
+  if (p.tile) {
     auto split = [&](auto zero) {
       using T = decltype(zero);
-      hipLaunchKernelGGL((split_columns_kernel<T>), dim3(static_cast<unsigned>((a.t + kUnitRows - 1) / kUnitRows + slices)),
-                         dim3(kSplitT), 0, s, static_cast<const T*>(a.x), a.ldx, a.x_scales, a.x_group, a.m, a.t, lo ? 2 : 1,
-                         a.centers, per_expert, units, exps, tops);
+      auto launch = [&](auto rows) {
+        constexpr int ROWS = decltype(rows)::value;
+        hipLaunchKernelGGL((split_columns_kernel<ROWS, T>), dim3(static_cast<unsigned>((a.t + ROWS - 1) / ROWS + slices)),
+                           dim3(kSplitT), 0, s, static_cast<const T*>(a.x), a.ldx, a.x_scales, a.x_group, a.m, a.t, lo ? 2 : 1,
+                           a.centers, per_expert, units, exps, tops);
+      };
+      if (a.t < kManyRows) launch(std::integral_constant<int, 2>());
+      else launch(std::integral_constant<int, 8>());
       return hipGetLastError();
     };
     e = a.x_dtype == KASHIN_E4M3 ? split(e4m3_t()) : with_float_type(a.x_dtype, split);
     if (e != hipSuccess) return e;
-    const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.per_group) * a.groups * 2 * p.splits),
-                    static_cast<unsigned>(p.tiles));
-    if (lo) hipLaunchKernelGGL((columns_tile_kernel<true>), grid, dim3(512), 0, s, a, p, units, exps, tops, parts);
-    else hipLaunchKernelGGL((columns_tile_kernel<false>), grid, dim3(512), 0, s, a, p, units, exps, tops, parts);
-    e = hipGetLastError();
+    e = p.tile == 64 ? (lo ? launch_columns_tile<64, true>(a, p, units, exps, tops, parts, s)
+                           : launch_columns_tile<64, false>(a, p, units, exps, tops, parts, s))
+                     : (lo ? launch_columns_tile<128, true>(a, p, units, exps, tops, parts, s)
+                           : launch_columns_tile<128, false>(a, p, units, exps, tops, parts, s));
   } else if (lo) {
     e = p.j == 0   ? launch_columns<0, true>(a, p, parts, s)
         : p.j == 1 ? launch_columns<1, true>(a, p, parts, s)
@@ -1420,9 +1439,11 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
   const int64_t each = rows_each(a.t, a.experts);
   const bool lo = a.y_dtype != KASHIN_BF16;
   const int parts = lo ? 2 : 1;
-  // Up to 63 rows P writes the operands itself; for many rows its 32-byte pieces of them cost more than a pass of their own.
-  // Where a row has several groups, each pair of them looks for the row's largest entry, at most 2^23 entries in all.
-  const bool direct = a.t < 64 && (a.groups == 1 || a.t * a.groups * k <= int64_t(1) << 23);
+  // P writes the operands itself: one launch and no P x in memory (4096 x 4096, bf16, 16 rows of x 22.9 -> 19.5 us against a
+  // pass of its own over x and P x, 2048 rows 198 -> 178; 64 experts 1000 x 2048, 4000 rows 119 -> 102).  Where a row has
+  // several groups each pair of them looks for the row's largest entry, so up to 2^22 entries looked at in all (rows of 16
+  // groups of 256: 16 rows of x 18.8 -> 14.5 us, 63 rows 28.9 -> 24.3; 100 rows 26.4 -> 27.0).
+  const bool direct = a.groups == 1 || a.t * a.groups * k <= int64_t(1) << 22;
   // the caller's rows where the next kernel can read them, else fp32 ones
   XRows x = {a.x, a.ldx, a.x_dtype};
   hipError_t e = hipSuccess;
@@ -1444,12 +1465,12 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
   e = apply_p(a, x, px, s);
   if (e != hipSuccess) return e;
 
-  if (a.t >= 64)
+  if (a.t >= kManyRows)
     hipLaunchKernelGGL((split_rows_kernel<8>), dim3(static_cast<unsigned>((a.t + 7) / 8)), dim3(kSplitT), 0, s, x, px, a.n,
                        a.groups, a.t, parts, frags, exps);
   else
-    hipLaunchKernelGGL((split_rows_kernel<1>), dim3(static_cast<unsigned>(a.t)), dim3(kSplitT), 0, s, x, px, a.n, a.groups, a.t,
-                       parts, frags, exps);
+    hipLaunchKernelGGL((split_rows_kernel<2>), dim3(static_cast<unsigned>((a.t + 1) / 2)), dim3(kSplitT), 0, s, x, px, a.n,
+                       a.groups, a.t, parts, frags, exps);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   return launch_product_rows(a, frags, exps, each, lo, s);
