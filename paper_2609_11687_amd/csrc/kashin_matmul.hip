@@ -213,9 +213,10 @@ __device__ __forceinline__ uint4_t load_codes(const uint8_t* group, int nby, int
 }
 
 // ------------------------------------------------------------------ x W^T: x and P x as operands
-// A workgroup takes ROWS rows (8: the lanes of eight rows write 128 consecutive bytes; 2 below kManyRows, to spread them
-// over the chip: the product of 4096 x 4096 with 128 rows of x 45.7 -> 35.4 us, 1024 rows 151 -> 145, 2000 rows 195.6 ->
-// 197.2), a thread 16 entries of a row at a time: two units.
+// For rows of many groups (kashin_layer_impl.h writes the operands of others).  A workgroup takes ROWS rows (8: the lanes
+// of eight rows write 128 consecutive bytes; 2 below kManyRows, to spread them over the chip: 4096 matrix rows, 16 groups of
+// 256, 128 rows of x 43.8 -> 33.9 us, 1024 rows 172.7 -> 167.7, 1536 rows 186.4 -> 187.8), a thread 16 entries of a row at a
+// time: two units.
 constexpr int kSplitT = 512;
 constexpr int kManyRows = 1536;
 template <int ROWS>
@@ -944,8 +945,8 @@ using short4_t = short __attribute__((ext_vector_type(4)));
 
 __host__ __device__ inline int64_t column_units(int64_t m) { return (m + kColsM - 1) / kColsM * (kColsM / 8); }
 
-// x as such units: a workgroup takes ROWS rows (as split_rows_kernel), and behind those workgroups kTopSlices look
-// through an expert's centres each.
+// x as such units: a workgroup takes ROWS rows (as split_rows_kernel: 509 bf16 rows of 11008, 24.3 us with 8 and 11.7 with
+// 2), and behind those workgroups kTopSlices look through an expert's centres each.
 template <int ROWS, class T>
 __global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int64_t ldx, const float* scales, int group, int64_t m,
                                                                 int64_t t, int parts, const float* centers, int64_t per_expert,
@@ -1441,9 +1442,10 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
   const int parts = lo ? 2 : 1;
   // P writes the operands itself: one launch and no P x in memory (4096 x 4096, bf16, 16 rows of x 22.9 -> 19.5 us against a
   // pass of its own over x and P x, 2048 rows 198 -> 178; 64 experts 1000 x 2048, 4000 rows 119 -> 102).  Where a row has
-  // several groups each pair of them looks for the row's largest entry, so up to 2^22 entries looked at in all (rows of 16
-  // groups of 256: 16 rows of x 18.8 -> 14.5 us, 63 rows 28.9 -> 24.3; 100 rows 26.4 -> 27.0).
-  const bool direct = a.groups == 1 || a.t * a.groups * k <= int64_t(1) << 22;
+  // several groups each pair of them looks for the row's largest entry: up to 2^28 entries looked at in all (4096 matrix rows;
+  // 16 groups of 256: one row of x 18.0 -> 13.8 us, 1000 rows 125 -> 122; 64 groups of 256: 100 rows, 2^27, 84 -> 76, 1000
+  // rows, 2^30, 453 -> 478).
+  const bool direct = a.groups == 1 || a.t * a.groups * k <= int64_t(1) << 28;
   // the caller's rows where the next kernel can read them, else fp32 ones
   XRows x = {a.x, a.ldx, a.x_dtype};
   hipError_t e = hipSuccess;

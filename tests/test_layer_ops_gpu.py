@@ -211,6 +211,12 @@ def _check(case, got, x, out, back, e=0):
         room = room + 33 * 2.0 ** -11 * (spread(ax @ case.top[0][e]) if case.rot is not None else ax @ case.top[0][e])
         room = room + 33 * 2.0 ** -11 * spread(ax @ case.top[1][e])
         norm += 3 * 2.0 ** -11
+    if not back and case.k > 2 ** 15:
+        # The quadratic sum above is of K up to 2^15.  An accumulator takes an eighth of the 2 K entries, 32 at a time, in
+        # three products: L = 6 K / 256 additions, each off by 2^-24 / sqrt(3) of a partial sum which grows as the root of
+        # its terms, sum_i i / L = L / 2: 2^-24 sqrt(L / 6) = 2^-24 sqrt(K / 256) of a typical result.  Four times that: the
+        # norm is of a few results only, which may be smaller than typical.
+        norm += 4 * 2.0 ** -24 * math.sqrt(case.k / 256)
     d = np.abs(_f64(got) - want)
     assert (d <= HALF_STEP[out] * np.abs(want) + room + LEAST[out]).all(), \
         (d / (HALF_STEP[out] * np.abs(want) + room + LEAST[out])).max()
@@ -283,6 +289,45 @@ def test_products_of_many_rows(n, groups, m, t, back):
     for dtype, out in (("bf16", "bf16"), ("f32", "f32")):
         x, y = _product(case, t, dtype, out, back)
         _check(case, y, x, out, back)
+
+
+@pytest.mark.parametrize("n,groups,m,t", [(64, 4096, 3, 1), (64, 4096, 3, 5), (64, 64, 5, 1601), (96, 48, 20, 700)])
+def test_products_of_rows_of_many_groups(n, groups, m, t):
+    print(f"product n={n} groups={groups} m={m} t={t}", flush=True)
+    case = Case(n, m, groups)
+    for dtype, out, xg in (("bf16", "bf16", 0), ("e4m3", "f32", 96), ("f32", "f16", 0)):
+        x, y = _product(case, t, dtype, out, False, xg, None if t > 5 else case.k + 3)
+        _check(case, y, x, out, False)
+
+
+@pytest.mark.parametrize("n,groups", [(172, 5), (512, 3), (4096, 1)])
+@pytest.mark.parametrize("x_group", [32, 96, 160, 4096])
+def test_products_of_scales_across_groups(n, groups, x_group):
+    """Scales of x whose entries begin and end inside a group of the codes, in both directions."""
+    for back in (False, True):
+        case = Case(n, 300, groups)
+        for t in (1, 2, 70):
+            x, y = _product(case, t, "e4m3", "f32", back, x_group)
+            _check(case, y, x, "f32", back)
+
+
+def test_rows_that_are_not_finite_keep_to_themselves():
+    """A row of several groups, or of e4m3 scales, next to rows that share its workgroups: they stay right."""
+    for n, groups in ((256, 3), (172, 1), (64, 5)):
+        case = Case(n, 30, groups)
+        x = _rows(np.random.default_rng(n), 9, case.k, "f16")
+        q, scales = x.to(torch.float8_e4m3fn), torch.ones((9, 1), device="cuda")
+        y = torch.empty((9, 30), device="cuda")
+        x[4, case.k - 1] = math.inf
+        K.kashin_matmul(case.plan, *case.dev, x, y, case.work(9, False))
+        others = [i for i in range(9) if i != 4]
+        _check(case, y[others], _f64(x[others]), "f32", False)
+        assert y[4].isnan().all()
+        scales[2] = math.nan
+        K.kashin_matmul(case.plan, *case.dev, q, y, case.work(9, False), scales)
+        others = [i for i in range(9) if i != 2]
+        _check(case, y[others], _f64(q[others]), "f32", False)
+        assert y[2].isnan().all()
 
 
 @pytest.mark.parametrize("back", [False, True])
