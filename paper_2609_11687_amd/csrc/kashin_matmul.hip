@@ -1409,15 +1409,26 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
 hipError_t launch_product_rows(const ProductArgs& a, const _Float16* frags, const int32_t* exps, int64_t each, bool lo,
                                hipStream_t s) {
   if (each <= 8 && lo) return launch_rows<0, 1, true>(a, frags, exps, s);
-  if (each <= 16) return lo ? launch_rows<1, 1, true>(a, frags, exps, s) : launch_rows<1, 1, false>(a, frags, exps, s);
-  // enough tiles of 256 x 128, or 256 x 64, to fill half the chip
+  // Few workgroups: smaller tiles.  16 x 16 up to 384 workgroups of them, 32 x 32 up to 256 (k = 4096, fp16 results, us with
+  // 16 x 16, 32 x 32 and 32 x 64: m = 72 with 300 rows of x, 95 workgroups, 29 36 46; with 1255, 395, 87 75 82; with 4000, 375 of
+  // 32 x 32, 238 206 204; m = 2000 with 40 rows, 375, 26 29 36; with 100, 875 and 252, 44 36 42).
+  const int64_t small = (a.m + 15) / 16 * ((a.t + 15) / 16), middle = (a.m + 31) / 32 * ((a.t + 31) / 32);
+  if (each <= 16 || small <= 384) return lo ? launch_rows<1, 1, true>(a, frags, exps, s) : launch_rows<1, 1, false>(a, frags, exps, s);
+  // Enough tiles of 256 x 128, or 256 x 64, to fill half the chip; the whole chip up to 48 rows of x a matrix, which leave
+  // much of a tile empty.  Experts' rows end inside a tile, so theirs are of 64 rows up to 192 a matrix (bf16 results, us with these
+  // tiles and with the next smaller: 32 experts, 2048 x 4096, 256 tiles: 30 rows each 94 and 138, 18 rows 90 and 103;
+  // 8 experts, 4096 x 4096, 128 tiles: 60 rows each 83 and 109, 40 rows 81 and 75; 64 and 128 rows: 32 experts, 130 rows each
+  // 246 and 278, 190 rows 351 and 354).
   const int64_t row_tiles = (a.m + kTileM - 1) / kTileM;
-  if (each >= 96 && row_tiles * (a.t / 128) >= 128)
+  const bool grouped = a.offsets != nullptr;
+  const int64_t tiles = grouped ? a.t / each * ((each + 63) / 64) : a.t / 64;
+  if (each >= (grouped ? 192 : 96) && row_tiles * (a.t / 128) >= 128)
     return lo ? launch_rows_tile<128, true>(a, frags, exps, s) : launch_rows_tile<128, false>(a, frags, exps, s);
-  if (each > 32 && row_tiles * (a.t / 64) >= 128)
+  if (row_tiles * tiles >= (each > 48 ? 128 : 256))
     return lo ? launch_rows_tile<64, true>(a, frags, exps, s) : launch_rows_tile<64, false>(a, frags, exps, s);
-  if (lo) return each <= 32 ? launch_rows<2, 2, true>(a, frags, exps, s) : launch_rows<4, 2, true>(a, frags, exps, s);
-  return each <= 32 ? launch_rows<2, 2, false>(a, frags, exps, s) : launch_rows<4, 2, false>(a, frags, exps, s);
+  if (each <= 32 || middle <= 256)
+    return lo ? launch_rows<2, 2, true>(a, frags, exps, s) : launch_rows<2, 2, false>(a, frags, exps, s);
+  return lo ? launch_rows<4, 2, true>(a, frags, exps, s) : launch_rows<4, 2, false>(a, frags, exps, s);
 }
 
 }  // namespace
