@@ -345,12 +345,14 @@ int64_t kashin_matmul_workspace_bytes(int32_t n, int64_t m, int32_t groups, int6
  *   x         t rows of k, dtype KASHIN_F32, _F16, _BF16 or _E4M3, ldx >= k (device)
  *   x_scales  KASHIN_E4M3: t x ceil(k / x_group) fp32 scales (x_group a multiple of 32), or t (x_group 0: one
  *             for each row); else null and x_group 0 (device)
- *   y         t rows of m, y_dtype KASHIN_F32, _F16 or _BF16, ldy >= m (device); overlaps neither x nor work
+ *   y         t rows of m, y_dtype KASHIN_F32, _F16 or _BF16, ldy >= m (device); neither y nor work overlaps
+ *             another argument
  *   work      at least kashin_matmul_workspace_bytes(n, m, groups, t, experts, 0) bytes, 16-byte aligned
  *             (device; its contents on entry do not matter; calls that overlap in time need one each)
- * P x and sums are fp32; the products are exact to about 2^-21 of a row's largest terms, where y is
- * bf16 to 2^-11 of each term (its operands are rounded to fp16).  A row of x holding NaN or Inf gives a row of NaN, a row of W_hat with a
- * centre that is not finite gives a column of NaN. */
+ * P x and sums are fp32; the products' operands are exact to about 2^-21 of a row's largest terms.  Where y is
+ * bf16 they are rounded to fp16: 2^-11 of each term (up to 33 * 2^-11 of |x| max|centre| a term, typically 3,
+ * transposed with fewer than 48 rows a matrix).  A row of x holding NaN or Inf gives a row of NaN, a row of W_hat
+ * with a centre that is not finite gives a column of NaN (transposed: the columns of its group). */
 int kashin_matmul(const kashin_weights* w, const void* x, int32_t x_dtype, int64_t t, int64_t ldx, const float* x_scales,
                   int32_t x_group, void* y, int32_t y_dtype, int64_t ldy, void* work, int64_t work_bytes, void* stream);
 

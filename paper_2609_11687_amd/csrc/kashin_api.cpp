@@ -778,6 +778,12 @@ int product(const kashin_weights* w, const int64_t* offsets, bool grouped, bool 
                 (long long)work_bytes);
   const Span sx(x, t, ldx, wx, elem_size(x_dtype)), sy(y, t, ldy, wy, elem_size(y_dtype)), sw(work, 1, 0, need, 1);
   if (sy.meets(sx) || sy.meets(sw) || sx.meets(sw)) return fail(KASHIN_E_INVALID, "x, y and work overlap");
+  const int64_t wrows = int64_t(w->experts) * w->m * w->groups;
+  const Span read[] = {{w->codes_u, 1, 0, wrows * (p->n / 4), 1}, {w->codes_v, 1, 0, wrows * (p->n / 4), 1},
+                       {w->centers, 1, 0, wrows * 8, 4}, {grouped ? offsets : nullptr, 1, 0, int64_t(w->experts) + 1, 8},
+                       {x_scales, 1, 0, t * (x_group ? (wx + x_group - 1) / x_group : 1), 4}};
+  for (const Span& r : read)
+    if (sy.meets(r) || sw.meets(r)) return fail(KASHIN_E_INVALID, "y or work overlaps codes, centers, offsets or scales");
   kashin::ProductArgs a;
   a.p = base_args(p, kashin::MODE_APPLY_P);
   a.n = p->n;

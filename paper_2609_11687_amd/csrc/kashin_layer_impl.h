@@ -76,7 +76,7 @@ __global__ __launch_bounds__(C::T) __attribute__((amdgpu_waves_per_eu(C::W))) vo
     vec[w].at = vec[w].g * N;
     vec[w].x = static_cast<const T*>(a.x) + vec[w].row * a.ldx + vec[w].at;
     if constexpr (E4M3)
-      vec[w].scales = a.x_scales + vec[w].row * (a.x_group ? (a.groups * N + a.x_group - 1) / a.x_group : 1);
+      vec[w].scales = a.x_scales + vec[w].row * (a.x_group ? (static_cast<int64_t>(a.groups) * N + a.x_group - 1) / a.x_group : 1);
   }
   // entries i .. i + 7 of a vector's row (i from the vector's first), those from `left` on as zero
   auto load_eight = [&](const LayerVector<T>& v, int i, int left, float* to) {
@@ -220,7 +220,8 @@ __global__ __launch_bounds__(C::T) __attribute__((amdgpu_waves_per_eu(C::W))) vo
   }
 }
 
-// y = zu + P zv: the end of the transposed products.  A workgroup walks pairs of vectors; a vector passes through LDS into
+// y = zu + P zv: the end of the transposed products (one row of 4096: 11 us, 509 rows 16; reading zu and zv and writing y would
+// take 4 us there, the transform's latency of a pair a compute unit the rest).  A workgroup walks pairs of vectors; a vector passes through LDS into
 // row order, where zu is added and y written in 16-byte pieces.
 template <class C>
 __global__ __launch_bounds__(C::T) __attribute__((amdgpu_waves_per_eu(C::W))) void layer_back_kernel(LayerBackArgs a) {

@@ -286,6 +286,9 @@ __global__ __launch_bounds__(kSplitT) void split_rows_kernel(XRows x, const floa
 // rows, whose hi parts are B's columns 0 .. 7 and lo parts columns 8 .. 15, so that two instructions give all four products
 // (against three for 16 rows).  LO: both operands in two parts; without it (J > 0) in one.  ALIGNED: n is a multiple of 256, so
 // that a slab lies in one group and no chunk is short: addresses and branches are scalar then.
+// One row of x, 11008 x 4096: 22.5 MB of codes in 12.5 us (1.8 TB/s; 4.4 us at the rate of a copy).  Bound by the decoding
+// (four byte selections for eight values, every instruction in a wave's own time) and by what a launch of eight waves a
+// workgroup waits for first: the centres' scale and the joining of the waves' sums.
 template <int J>
 constexpr int tile_rows() { return J == 0 ? 8 : 16 * J; }
 
@@ -488,17 +491,22 @@ __global__ __launch_bounds__(kRowsT, 2) void rows_kernel(ProductArgs a, const _F
 }
 
 // y = x W^T for many rows of x: a workgroup computes 256 matrix rows by TT rows of x in 32 x 32 tiles: 128 rows of x, wave
-// (rw, cw) 64 by 64 of them, or 64, a wave 32 by 64.  The rows of x pass through LDS (128 entries of K of one factor at a time, two buffers, filled by loads
-// that go to LDS directly); a wave decodes its matrix rows' codes in registers, each code once for 64 rows of x.
+// (rw, cw) 64 by 64 of them, or 64, a wave 32 by 64.  The rows of x pass through LDS (128 entries of K of one factor at a
+// time, two buffers, filled by loads that go to LDS directly); a wave decodes its matrix rows' codes in registers, each code
+// once for 64 rows of x.
 using float16_t = float __attribute__((ext_vector_type(16)));
 constexpr int kTileM = 256;
 
-// 16 bytes a lane from memory to LDS, lane by lane behind `lds` (the same in all lanes).  Written as an instruction: the
+// 16 bytes a lane from memory to LDS, lane by lane behind `lds`; `from` and `lds` are the same in all lanes, `off` is the lane's
+// offset in bytes.  Written as an instruction: the
 // compiler would let every later LDS read wait for it, also of the other buffer.  It has no register output; who reads the
 // data waits with wait_loads first, then at a barrier (which alone does not wait).
-__device__ __forceinline__ void load_to_lds(const void* from, const void* lds) {
+__device__ __forceinline__ void load_to_lds(const void* from, uint32_t off, const void* lds) {
   const int at = uniform(static_cast<int>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)lds)));
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(at) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :
+               : "v"(off), "s"(from), "s"(at)
+               : "memory", "m0");
 }
 // Until at most N of this wave's loads are under way (they arrive in order).
 template <int N>
@@ -506,8 +514,9 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-// Two workgroups a unit where hi parts alone leave room for it (64 KB of LDS, 128 registers, three of them
-// spilled): 426 us against 455 with one, 2048 rows of x, 11008 x 4096.
+// Two workgroups a unit where hi parts alone leave room for it (65 KB of LDS, 128 registers).  Bound by the matrix
+// instructions: 2048 rows of x, 11008 x 4096, bf16 result, 369 GFLOP of [x | P x] [U | V]^T in 393 us, 940 TFLOP/s
+// (one workgroup a unit and addresses of 64 bits for x 455).
 template <int TT, bool LO, bool ALIGNED>
 __global__ __launch_bounds__(512, LO || !ALIGNED ? 2 : 4) void rows_tile_kernel(ProductArgs a, const _Float16* frags, const int32_t* exps) {
   constexpr int PARTS = LO ? 2 : 1, SU = 2 * kUnits;  // units of a slab: two chunks
@@ -547,16 +556,17 @@ __global__ __launch_bounds__(512, LO || !ALIGNED ? 2 : 4) void rows_tile_kernel(
         c[i] = load_codes(base + static_cast<uint32_t>((crow[i] + g) * static_cast<uint32_t>(nby)), nby, (at - g * cpg) * 16);
     }
   };
+  const int mine_x = (wave % RT) * 64 + lane;  // this lane's row of x in a load (past the last repeats it)
+  const uint32_t x_off = static_cast<uint32_t>(tl.row0 + (mine_x < tl.rows ? mine_x : tl.rows - 1)) * 16u;
   auto fill = [&](int it, int buf) {  // a wave's load takes 64 rows of x of a unit
-    const int f = it >= slabs, c = (wave % RT) * 64 + lane;
+    const int f = it >= slabs;
     const int64_t u0 = f * units + static_cast<int64_t>(it - f * slabs) * SU;
-    const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
 #pragma unroll
     for (int pt = 0; pt < PARTS; ++pt)
 #pragma unroll
       for (int k = 0; k < SU * RT / 8; ++k) {
         const int u = 8 / RT * k + wave / RT;
-        load_to_lds(frags + (((u0 + u) * PARTS + pt) * a.t + row) * 8, &xs[buf][pt][u][(wave % RT) * 64][0]);
+        load_to_lds(frags + ((u0 + u) * PARTS + pt) * a.t * 8, x_off, &xs[buf][pt][u][(wave % RT) * 64][0]);
       }
   };
   // codes are loaded two items ahead: an item takes less time than memory does
@@ -682,7 +692,9 @@ __global__ __launch_bounds__(512, LO || !ALIGNED ? 2 : 4) void rows_tile_kernel(
 // take a shift and three ands.
 //
 // A workgroup scales by what it meets: max |x| of a row of x into [2^6, 2^7), the largest finite centre into [2^4, 2^5), so
-// that a coefficient times x stays below 2^14.
+// that a coefficient times x stays below 2^14.  Products of a bf16 result take the coefficients' hi parts only.
+// One row of x, 4096 x 4096: 8.4 MB of codes and 0.3 of centres in 11.3 us, and 3.5 us to join the splits; bound by the loads'
+// latency over the 32 steps of a workgroup, of which three are under way.
 constexpr int kTopSlices = 16;  // partial maxima of an expert's centres (the tiled kernel's)
 
 // The caller's rows of x.
@@ -940,6 +952,9 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
 // eight matrix rows).  A dword's codes lie in LDS in the order they come out of the tables, 0 4 8 12 1 5 9 13 ..: column
 // 16 d + p / 4 + 4 (p % 4) at place p, which the stores undo.
 // x comes as units of eight matrix rows: units[part][unit][row of x][8], scaled as for x W^T.
+// 509 rows of x, 11008 x 4096, bf16 result: 92 GFLOP in 122 us, 750 TFLOP/s (128-row tiles, two workgroups a unit: 142 us
+// with the two registers more that leave room for one); bound by the LDS traffic of the decoded codes beside the matrix
+// instructions.
 constexpr int kColsM = 32, kColsN = 256, kColsLd = kColsN + 32;  // 576-byte rows: four of them on 64 banks
 using short4_t = short __attribute__((ext_vector_type(4)));
 
@@ -1019,7 +1034,7 @@ __global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int6
 }
 
 template <int TT, bool LO>
-__global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, ColumnsPlan pl, const _Float16* units,
+__global__ __launch_bounds__(512, LO ? 2 : 4) void columns_tile_kernel(ProductArgs a, ColumnsPlan pl, const _Float16* units,
                                                               const int32_t* exps, const uint32_t* tops, float* out) {
   constexpr int PARTS = LO ? 2 : 1, I = TT / 64;
   __shared__ __align__(16) _Float16 ws[2][PARTS][kColsM][kColsLd];
@@ -1076,14 +1091,15 @@ __global__ __launch_bounds__(512, 2) void columns_tile_kernel(ProductArgs a, Col
     }
   };
   const int64_t all = column_units(a.m);
+  const int mine_x = 64 * (wave % I) + lane;  // this lane's row of x in a load (past the last repeats it)
+  const uint32_t x_off = static_cast<uint32_t>(tl.row0 + (mine_x < tl.rows ? mine_x : tl.rows - 1)) * 16u;
   auto fill = [&](int64_t k0, int buf) {
     constexpr int PIECES = PARTS * (kColsM / 8) * I;  // of 64 rows: a wave's load
 #pragma unroll
     for (int p0 = 0; p0 < PIECES; p0 += 8) {
-      const int p = p0 + wave, h = p % I, u = p / I % (kColsM / 8), pt = p / I / (kColsM / 8), c = 64 * h + lane;
+      const int p = p0 + wave, u = p / I % (kColsM / 8), pt = p / I / (kColsM / 8);
       if (PIECES < 8 && p >= PIECES) break;
-      const int64_t row = tl.row0 + (c < tl.rows ? c : tl.rows - 1);
-      load_to_lds(units + ((pt * all + k0 / 8 + u) * a.t + row) * 8, &xs[buf][pt][u][64 * h][0]);
+      load_to_lds(units + (pt * all + k0 / 8 + u) * a.t * 8, x_off, &xs[buf][pt][u][64 * (wave % I)][0]);
     }
   };
   float16_t acc[I][2];

@@ -5,6 +5,9 @@
 // over (entry (c NT + tid) 8 + j), so that a group of 32 .. 256 entries is 4 .. 32 neighbouring lanes and its
 // maximum a few shuffles.  The sum of squares is fp32: eight entries in a thread, the wave by shuffles, the
 // waves through LDS in a fixed order, so that results repeat bit for bit.
+//
+// Bound by memory: 8192 bf16 rows of 8192 with r and h (537 MB) take 102 us, 5.2 TB/s against 5.1 of a
+// large copy; one row of 4096 is 4 us, the launch.
 #include "kashin_internal.h"
 #include "kashin_rows.h"
 
@@ -27,7 +30,7 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes) {
   return v;
 }
 
-// Threads of a row: 64 (four rows a workgroup), 256 or 1024.
+// NT threads of a row: 64 (four rows a workgroup) to 1024.
 template <class T, int NT, int C>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_kernel(NormArgs a) {
   constexpr int RPW = NT < 256 ? 256 / NT : 1;  // rows a workgroup
@@ -166,12 +169,17 @@ hipError_t launch_as(const NormArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_rmsnorm(const NormArgs& a, int dtype, hipStream_t stream) {
+  // The fewest threads that hold the row in eight entries each, so that all its loads are under way at once, and short rows
+  // four to a workgroup (16384 bf16 rows with e4m3 output, us: 512 wide 64 threads 16 and 256 threads 37; 2048 wide 256
+  // threads 48 and 64 of 32 entries 56); from 4097 on two eights, which leave room for three rows a compute unit and more
+  // (8192 wide 512 threads 216 and 1024 277; 16384 wide 1024 threads 538, 512 of 32 entries 517, but one pass over 64 rows 8.7
+  // and 10.3).
   return with_float_type(dtype, [&](auto zero) {
     using T = decltype(zero);
     if (a.n <= 512) return launch_as<T, 64, 1>(a, stream);
     if (a.n <= 2048) return launch_as<T, 256, 1>(a, stream);
     if (a.n <= 4096) return launch_as<T, 512, 1>(a, stream);
-    if (a.n <= 8192) return launch_as<T, 1024, 1>(a, stream);
+    if (a.n <= 8192) return launch_as<T, 512, 2>(a, stream);
     return launch_as<T, 1024, 2>(a, stream);
   });
 }

@@ -631,3 +631,25 @@ def test_product_refusals_with_a_plan():
     empty = (None, 0, 0, n, None, 0, None, 0, 4, None, 0, None)
     assert L.kashin_matmul(ctypes.addressof(w), *empty) == K.KASHIN_OK
     K.kashin_matmul(case.plan, *case.dev, x[:0], y[:0], work[:0])
+
+
+def test_outputs_over_other_arguments_are_refused():
+    case = Case(512, 6, experts=2)
+    cu, cv, ce = case.dev
+    x, y = torch.zeros((4, 512), device="cuda"), torch.zeros((4, 6), device="cuda")
+    off = torch.tensor([0, 2, 4], device="cuda")
+    work = case.work(4, False)
+    before = [a.clone() for a in (cu, cv, ce, off)]
+    q = x.to(torch.float8_e4m3fn)
+    for over in (cu.view(-1)[:96].view(torch.float32).view(4, 6), ce.view(-1)[8:32].view(4, 6)):
+        with pytest.raises((K.KashinError, ValueError), match="overlap"):
+            K.kashin_matmul_experts(case.plan, cu, cv, ce, off, x, over, work, False)
+    big = torch.zeros(work.numel() + 4096, dtype=torch.uint8, device="cuda")
+    inside = big[256:272].view(torch.float32).view(4, 1)
+    with pytest.raises((K.KashinError, ValueError), match="overlap"):
+        K.kashin_matmul_experts(case.plan, cu, cv, ce, off, q, y, big, False, inside)
+    o2 = big[512:536].view(torch.int64)
+    with pytest.raises((K.KashinError, ValueError), match="overlap"):
+        K.kashin_matmul_experts(case.plan, cu, cv, ce, o2, x, y, big, False)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(before, (cu, cv, ce, off)))
