@@ -122,8 +122,6 @@ __global__ __launch_bounds__(256) void widen_kernel(const T* x, int64_t ldx, con
   store8(out + row * width + i, valid, v);
 }
 
-__device__ __forceinline__ float pick(const float* q, int c) { return c & 2 ? (c & 1 ? q[3] : q[2]) : (c & 1 ? q[1] : q[0]); }
-
 __device__ __forceinline__ void put(void* y, int dtype, int64_t i, float v) {
   if (dtype == KASHIN_F32) static_cast<float*>(y)[i] = v;
   else if (dtype == KASHIN_F16) static_cast<_Float16*>(y)[i] = static_cast<_Float16>(v);
@@ -766,7 +764,7 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
   // Codes, and a thread's first item of operand B, are loaded AHEAD steps ahead: a step takes less time than memory does.
   // Loads past the last matrix row take that row again.
   // Item it = (it % 16, it / 16) = (pair of matrix rows, row of x).
-  constexpr int AHEAD = J <= 1 ? 3 : 1;
+  constexpr int AHEAD = 3;
   struct Item {
     float x[2];
     float4_t ce[2];
@@ -1284,8 +1282,8 @@ ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, b
   for (p.waves = 8; p.waves > 1; p.waves /= 2)  // at most an eighth of the waves idle
     if (((blocks + p.waves - 1) / p.waves * p.waves - blocks) * 8 <= blocks) break;
   p.per_group = (blocks + p.waves - 1) / p.waves;
-  p.j = each <= 8 ? 0 : each <= 16 ? 1 : 2;
-  p.tiles = most_tiles(grouped, t, experts, p.j == 0 ? 8 : 16 * p.j);
+  p.j = each <= 8 ? 0 : 1;  // 8 rows of x: 36 us against 42 of the 16-row form, one row 25 and 27 (4096 x 4096, fp32)
+  p.tiles = most_tiles(grouped, t, experts, p.j == 0 ? 8 : 16);
   // enough workgroups of eight waves to fill the chip twice over, of at least 64 rows each
   const int64_t fill = 512 * 8 / p.waves, one = static_cast<int64_t>(p.per_group) * groups * 2;
   const int64_t tiles = p.tiles > 0 ? p.tiles : 1, most = (m + 63) / 64;
@@ -1293,14 +1291,16 @@ ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, b
   p.rows = ((m + splits - 1) / splits + 31) / 32 * 32;
   p.splits = static_cast<int>((m + p.rows - 1) / p.rows);
   // splits * t of this and of every smaller t (a workspace for t rows serves fewer): at most one split a 64 rows, and
-  // tiles of at most 32 rows each want their share of `fill`
-  const int64_t bound = (fill / one + 1) * 32 + t;
+  // tiles of at most 16 rows each want their share of `fill`
+  const int64_t bound = (fill / one + 1) * 16 + t;
   p.part_rows = most * t < bound ? most * t : bound;
-  // From 48 rows of x a matrix on, tiles.  Of 64 rows where 128 would be half empty; where experts' rows end in a tile's
-  // middle 64 also pay up to 128 rows a matrix with hi and lo parts, whose products hide the codes' decoding (8 experts, 2048 x
-  // 4096, fp32 results, us with 64 and 128: 400 rows 131 and 152, 700 rows 156 and 191, 1500 rows 288 and 248; bf16: 400
-  // rows 81 and 84, 700 rows 96 and 92).
-  p.tile = each < 48 ? 0 : (grouped ? each < (lo ? 128 : 64) : t <= 64) ? 64 : 128;
+  // Tiles from 16 rows of x a matrix on, with hi parts alone from 8 (4096 x 4096, us with and without: fp32 results 16 rows of
+  // x 45 and 59, 12 rows 44 and 39, 47 rows 50 and 83; bf16 8 rows 33 and 41, 4 rows 32 and 31; 8 experts, 2048 x 4096: fp32
+  // 16 rows each 88 and 83, 32 rows 90 and 124, bf16 8 rows 53 and 48, 10 rows 53 and 65).  Of 64 rows where 128
+  // would be half empty; where experts' rows end in a tile's middle 64 also pay up to 128 rows a matrix with hi and lo parts,
+  // whose products hide the codes' decoding (8 experts, 2048 x 4096, fp32 results, us with 64 and 128: 400 rows 131 and
+  // 152, 700 rows 156 and 191, 1500 rows 288 and 248; bf16: 400 rows 81 and 84, 700 rows 96 and 92).
+  p.tile = each < (lo ? 16 : 8) ? 0 : (grouped ? each < (lo ? 128 : 64) : t <= 64) ? 64 : 128;
   if (p.tile) {
     p.per_group = (n + kColsN - 1) / kColsN;
     p.tiles = most_tiles(grouped, t, experts, p.tile);
@@ -1391,11 +1391,9 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
                      : (lo ? launch_columns_tile<128, true>(a, p, units, exps, tops, parts, s)
                            : launch_columns_tile<128, false>(a, p, units, exps, tops, parts, s));
   } else if (lo) {
-    e = p.j == 0   ? launch_columns<0, true>(a, p, parts, s)
-        : p.j == 1 ? launch_columns<1, true>(a, p, parts, s)
-                   : launch_columns<2, true>(a, p, parts, s);
+    e = p.j == 0 ? launch_columns<0, true>(a, p, parts, s) : launch_columns<1, true>(a, p, parts, s);
   } else {
-    e = p.j == 1 ? launch_columns<1, false>(a, p, parts, s) : launch_columns<2, false>(a, p, parts, s);
+    e = launch_columns<1, false>(a, p, parts, s);
   }
   if (e != hipSuccess) return e;
   const unsigned rows = static_cast<unsigned>(a.t), strips = static_cast<unsigned>((k + 255) / 256);
@@ -1424,6 +1422,7 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
 // The product itself, by the rows that a matrix meets.
 hipError_t launch_product_rows(const ProductArgs& a, const _Float16* frags, const int32_t* exps, int64_t each, bool lo,
                                hipStream_t s) {
+  // 4096 x 4096, fp32: 8 rows of x 21.2 us against 22.3 of the 16-row form
   if (each <= 8 && lo) return launch_rows<0, 1, true>(a, frags, exps, s);
   // Few workgroups: smaller tiles.  16 x 16 up to 384 workgroups of them, 32 x 32 up to 256 (k = 4096, fp16 results, us with
   // 16 x 16, 32 x 32 and 32 x 64: m = 72 with 300 rows of x, 95 workgroups, 29 36 46; with 1255, 395, 87 75 82; with 4000, 375 of
