@@ -1,0 +1,116 @@
+"""The layer operators' further forms on the GPU against float64: every vector length, every tile of the products whole and by
+expert, rows that no expert has.  Tolerances as in test_layer_ops_gpu, whose helpers these tests use; where one differs
+its derivation stands beside it."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import test_layer_ops_gpu as base
+from paper_2609_11687_amd import kashin as K
+from test_layer_ops_gpu import Case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    K.lib()
+
+
+# ----------------------------------------------------------------------------- lengths
+@pytest.mark.parametrize("back", [False, True])
+def test_products_of_every_compiled_length(back):
+    for n in (n for n in range(2, 20000, 2) if K.kashin_supported_n(n)):
+        print(f"product n={n} back={back}", flush=True)
+        case = Case(n, 37)
+        for t, dtype, out, xg in ((1, "e4m3", "f32", 64), (2, "f32", "f32", 0), (5, "f16", "f16", 0), (19, "e4m3", "bf16", 0),
+                                  (70, "bf16", "f32", 0)):
+            x, y = base._product(case, t, dtype, out, back, xg)
+            base._check(case, y, x, out, back)
+
+
+# ----------------------------------------------------------------------------- tiles
+@pytest.mark.parametrize("n,m,t", [(96, 1000, 130), (172, 1000, 130), (512, 1000, 130),  # 32 x 32
+                                   (96, 1000, 400), (172, 1000, 400), (512, 1000, 400),  # 32 x 64
+                                   (96, 8200, 100), (172, 8200, 250)])                   # 256 x 64, 256 x 128
+def test_products_of_every_tile(n, m, t):
+    print(f"product n={n} m={m} t={t}", flush=True)
+    case = Case(n, m)
+    for dtype, out in (("bf16", "bf16"), ("f16", "f16"), ("e4m3", "f32")):
+        x, y = base._product(case, t, dtype, out, False, 32 if dtype == "e4m3" else 0)
+        base._check(case, y, x, out, False)
+
+
+@pytest.mark.parametrize("n,groups,t", [(64, 128, 300), (64, 64, 1601)])
+def test_products_of_16_bit_rows_of_many_groups(n, groups, t):
+    """Rows whose P x passes through memory."""
+    case = Case(n, 5, groups)
+    for dtype, out in (("f16", "f32"), ("f16", "bf16"), ("bf16", "f16")):
+        x, y = base._product(case, t, dtype, out, False)
+        base._check(case, y, x, out, False)
+
+
+def _ragged(experts, each, seed):
+    """Row counts of `experts` experts, `each` on average, from none to three times that."""
+    rng = np.random.default_rng(seed)
+    share = rng.uniform(0.0, 3.0, experts) ** 2
+    share[experts // 2] = 0.0
+    return list(rng.multinomial(experts * each, share / share.sum()))
+
+
+def _grouped(case, counts, first, spare, dtype, out, back, seed=0):
+    """Products by expert, the rows outside the offsets' range holding NaN and infinities (scales too), against float64."""
+    rng = np.random.default_rng([seed, len(counts)])
+    used = int(sum(counts))
+    t = first + used + spare
+    wx, wy = (case.m, case.k) if back else (case.k, case.m)
+    x = base._rows(rng, t, wx, dtype)
+    scales = None
+    if dtype == "e4m3":
+        scales = torch.from_numpy(rng.uniform(0.1, 2.0, (t, 1)).astype(np.float32)).cuda()
+    x64 = base._f64(x) * (base._f64(scales) if scales is not None else 1.0)
+    for row in list(range(first)) + list(range(first + used, t)):
+        x[row] = math.nan
+        if dtype != "e4m3":
+            x[row, ::3] = math.inf
+            x[row, 1::3] = -math.inf
+        else:
+            scales[row] = math.inf if row % 2 else math.nan
+    off = first + np.concatenate([[0], np.cumsum(counts)])
+    flat, y = base._buffer(t, wy, out)
+    K.kashin_matmul_experts(case.plan, *case.dev, torch.from_numpy(off.astype(np.int64)).cuda(), x, y, case.work(t, back), back,
+                            scales, 0, rot_seed=case.rot)
+    torch.cuda.synchronize()
+    for e in range(case.experts):
+        base._check(case, y[off[e]:off[e + 1]], x64[off[e]:off[e + 1]], out, back, e)
+    f = flat.to(torch.float32)
+    assert (f[:first * wy] == 7).all() and (f[(first + used) * wy:] == 7).all()
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("n,groups,m,experts,each", [
+    (256, 2, 35, 5, 3), (96, 1, 70, 3, 12),
+    (256, 1, 1000, 8, 20), (96, 1, 1000, 8, 20),    # 32 x 32
+    (256, 1, 1200, 6, 45), (172, 1, 1200, 6, 45),   # 32 x 64
+    (64, 1, 1800, 32, 30), (256, 1, 300, 32, 130), (172, 1, 300, 32, 130),  # 256 x 64
+    (256, 1, 4100, 5, 250)])                        # 256 x 128
+def test_experts_of_every_tile(n, groups, m, experts, each, back):
+    print(f"experts {experts} of {each} n={n} m={m} back={back}", flush=True)
+    case = Case(n, m, groups, experts=experts)
+    counts = _ragged(experts, each, m)
+    for dtype, out in (("bf16", "bf16"), ("f32", "f32"), ("e4m3", "bf16")):
+        _grouped(case, counts, 3, 2, dtype, out, back)
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("n,groups,rot", [(512, 1, 3), (64, 3, 7)])
+def test_experts_of_rotated_weights_beside_rows_of_nobody(n, groups, rot, back):
+    for each in (4, 40):
+        case = Case(n, 90, groups, experts=4, rot=rot)
+        for dtype, out in (("f16", "f32"), ("e4m3", "bf16")):
+            _grouped(case, _ragged(4, each, n), 1, 3, dtype, out, back)
