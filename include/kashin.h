@@ -314,8 +314,10 @@ int kashin_optq_quantize_noalloc(kashin_plan_t plan, float* w_t, int64_t d_in, i
  *   y       t rows of y_dtype KASHIN_F32, _F16, _BF16 or _E4M3, ldy >= n (device); overlaps none of the others
  *   scales  t x ceil(n / group) fp32, or t for group 0 (device): KASHIN_E4M3 only, else null and group 0
  *   group   0, 32, 64, 128 or 256
- * Sums are fp32: a row whose sum of squares passes 3.4e38 gives zeros.  A row holding NaN or Inf gives NaN
- * where y is; in 8 bits, a group holding NaN has scale NaN and zeros.  A group of zeros has scale 0.
+ * Sums are fp32: a row whose sum of squares passes 3.4e38 gives zeros, and with eps = 0 one whose squares vanish
+ * (entries below about 1e-23) infinities, or NaN for its zeros.  A row holding NaN gives NaN, one holding Inf gives NaN there
+ * and zeros elsewhere.  In 8 bits, a group with a NaN or an infinite y (weight's too) has scale NaN and zeros.  A
+ * group of zeros has scale 0.
  * Plan-free: runs on the current device. */
 int kashin_rmsnorm(int64_t t, int32_t n, const void* x, int32_t dtype, int64_t ldx, const void* r, int64_t ldr,
                    const void* weight, float eps, void* h, int64_t ldh, void* y, int32_t y_dtype, int64_t ldy,

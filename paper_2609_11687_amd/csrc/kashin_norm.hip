@@ -145,10 +145,11 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void rmsnorm_kernel(NormArgs a
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int i = (c * NT + tid) * 8;
-      const float scale = __uint_as_float(tops[c]) / 448.f;
+      // a group with an infinite entry has no more a scale than one with a NaN
+      const float scale = tops[c] < 0x7f800000u ? __uint_as_float(tops[c]) / 448.f : __uint_as_float(0x7fc00000u);
       if (i < n && (a.group ? i % a.group == 0 : i == 0))
         a.scales[row * groups + (a.group ? i / a.group : 0)] = scale;
-      // zeros for a group of zeros (scale 0) and for one that holds NaN (scale NaN)
+      // zeros for a group of zeros (scale 0) and for one that is not finite (scale NaN)
       float q[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) q[j] = scale > 0.f ? fminf(fmaxf(s[c][j] / scale, -448.f), 448.f) : 0.f;

@@ -1,6 +1,6 @@
 """The layer operators' further forms on the GPU against float64: every vector length, every tile of the products whole and by
-expert, rows that no expert has.  Tolerances as in test_layer_ops_gpu, whose helpers these tests use; where one differs
-its derivation stands beside it."""
+expert, rows that no expert has, values that are not finite.  Tolerances as in test_layer_ops_gpu, whose helpers these
+tests use; where one differs its derivation stands beside it."""
 import math
 
 import numpy as np
@@ -20,6 +20,38 @@ def _need_gpu():
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     K.lib()
+
+
+# ----------------------------------------------------------------------------- norm
+@pytest.mark.parametrize("n", [300, 1024, 5000, 12000])
+@pytest.mark.parametrize("group", [0, 32, 128])
+def test_rmsnorm_groups_with_an_infinite_y(n, group):
+    """A group of 8-bit entries with an infinite one is a group that has no scale: scale NaN and zeros, as with a NaN."""
+    rng = np.random.default_rng(n + group)
+    x = torch.from_numpy(rng.standard_normal((6, n)).astype(np.float32)).cuda()
+    x[:, 5], x[:, 70] = 1.5, -1.5
+    x[4] *= 1e-25  # the squares underflow
+    x[5] = 0.0
+    w = torch.ones(n, device="cuda")
+    w[5], w[70] = math.inf, 3e38  # at 70 the product passes the largest float
+    cols = -(-n // group) if group else 1
+    for weight, eps in ((w, 1e-6), (None, 0.0)):
+        y = torch.empty((6, n), device="cuda")
+        q, s = torch.full((6, n), 7.0).to(torch.float8_e4m3fn).cuda(), torch.full((6, cols), 7.0, device="cuda")
+        K.kashin_rmsnorm(x, None, weight, eps, None, y)
+        K.kashin_rmsnorm(x, None, weight, eps, None, q, s, group)
+        torch.cuda.synchronize()
+        y, q, s = base._f64(y), base._f64(q), base._f64(s)
+        for g in range(cols):
+            part = slice(g * group, (g + 1) * group) if group else slice(0, n)
+            lost = ~np.isfinite(y[:, part]).all(1)
+            assert (q[lost][:, part] == 0).all() and np.isnan(s[lost, g]).all(), (g, q[lost][:, part], s[lost, g])
+            kept = y[~lost][:, part]
+            assert np.allclose(s[~lost, g], np.abs(kept).max(1, initial=0.0) / 448, rtol=2.0 ** -22, atol=0)
+            if eps == 0.0:
+                assert lost[4] and lost[5]
+            elif g == 0:
+                assert lost[:4].all()
 
 
 # ----------------------------------------------------------------------------- lengths
