@@ -693,7 +693,10 @@ __global__ __launch_bounds__(512, LO || !ALIGNED ? 2 : 4) void rows_tile_kernel(
 // that a coefficient times x stays below 2^14.  Products of a bf16 result take the coefficients' hi parts only.
 // One row of x, 4096 x 4096: 8.4 MB of codes and 0.3 of centres in 11.3 us, and 3.5 us to join the splits; bound by the loads'
 // latency over the 32 steps of a workgroup, of which three are under way.
-constexpr int kTopSlices = 16;  // partial maxima of an expert's centres (the tiled kernel's)
+// The tiled kernel's partial maxima of the centres: of each expert's groups and factors (a key: group * 2 + factor), over this
+// many slices of its matrix rows.
+constexpr int kTopSlices = 16;
+__host__ __device__ constexpr int top_slices(int64_t m) { return m < 512 ? static_cast<int>((m + 31) / 32) : kTopSlices; }
 
 // The caller's rows of x.
 template <class T>
@@ -959,32 +962,47 @@ using short4_t = short __attribute__((ext_vector_type(4)));
 __host__ __device__ inline int64_t column_units(int64_t m) { return (m + kColsM - 1) / kColsM * (kColsM / 8); }
 
 // x as such units: a workgroup takes ROWS rows (as split_rows_kernel: 509 bf16 rows of 11008, 24.3 us with 8 and 11.7 with
-// 2), and behind those workgroups kTopSlices look through an expert's centres each.
+// 2), and behind those workgroups each looks through a slice of an expert's matrix rows for the largest finite centre of
+// up to kSplitT keys, which lie behind each other in a matrix row's centres.
 template <int ROWS, class T>
 __global__ __launch_bounds__(kSplitT) void split_columns_kernel(const T* x, int64_t ldx, const float* scales, int group, int64_t m,
-                                                                int64_t t, int parts, const float* centers, int64_t per_expert,
+                                                                int64_t t, int parts, const float* centers, int keys,
                                                                 _Float16* units, int32_t* exps, uint32_t* tops) {
-  __shared__ uint32_t top_of[ROWS];
+  __shared__ uint32_t top_of[kSplitT];
   const int tid = threadIdx.x, mine = tid % ROWS;
   const int64_t row_blocks = (t + ROWS - 1) / ROWS;
-  if (tid < ROWS) top_of[tid] = 0;
+  top_of[tid] = 0;
   __syncthreads();
   uint32_t top = 0;
-  if (blockIdx.x >= row_blocks) {  // the largest finite centre of a slice of an expert's
-    const int64_t id = blockIdx.x - row_blocks, e = id / kTopSlices, slice = id % kTopSlices;
-    const float* ce = centers + e * per_expert;
-    for (int64_t i = (slice * kSplitT + tid) * 4; i < per_expert; i += kTopSlices * kSplitT * 4) {
-      const float4_t v = *reinterpret_cast<const float4_t*>(ce + i);
+  if (blockIdx.x >= row_blocks) {
+    const int slices = top_slices(m), key_blocks = (keys + kSplitT - 1) / kSplitT;
+    int64_t id = blockIdx.x - row_blocks;
+    const int first = static_cast<int>(id % key_blocks) * kSplitT, here = keys - first < kSplitT ? keys - first : kSplitT;
+    id /= key_blocks;
+    const int64_t e = id / slices, slice = id % slices;
+    const int rows = kSplitT / here, key = tid % here;  // matrix rows side by side; threads past the last whole one idle
+    if (tid < rows * here) {
+      const float* ce = centers + (e * m * keys + first + key) * 4;
+#pragma unroll 4
+      for (int64_t i = slice * rows + tid / here; i < m; i += static_cast<int64_t>(slices) * rows) {
+        const float4_t v = *reinterpret_cast<const float4_t*>(ce + i * keys * 4);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
-        top = b > top && b < kInfBits ? b : top;
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t b = __float_as_uint(v[j]) & 0x7fffffffu;
+          top = b > top && b < kInfBits ? b : top;
+        }
       }
     }
-    top = wave_max(top);
-    if (tid % 64 == 0) atomicMax(&top_of[0], top);  // a maximum: the same in any order
+    const bool fold = here < 64 && (here & (here - 1)) == 0;  // 64 lanes hold whole matrix rows: no two lanes on one address
+    if (fold) {
+      for (int d = here; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_xor(top, d);
+        top = o > top ? o : top;
+      }
+    }
+    if (tid < rows * here && (!fold || tid % 64 < here)) atomicMax(&top_of[key], top);  // a maximum: the same in any order
     __syncthreads();
-    if (tid == 0) tops[id] = top_of[0];
+    if (tid < here) tops[(e * keys + first + tid) * slices + slice] = top_of[tid];
     return;
   }
   const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + mine;
@@ -1049,10 +1067,13 @@ __global__ __launch_bounds__(512, LO ? 2 : 4) void columns_tile_kernel(ProductAr
   id /= a.groups;
   const int f = id % 2, split = id / 2;
   const int64_t i0 = split * pl.rows, i1 = i0 + pl.rows < a.m ? i0 + pl.rows : a.m;
+  // scaled by the largest centre of this group and factor, so that other groups' magnitudes do not matter
   uint32_t top = 0;
+  const int slices = top_slices(a.m);
+  const uint32_t* key_tops = tops + ((static_cast<int64_t>(tl.expert) * a.groups + g) * 2 + f) * slices;
 #pragma unroll
   for (int s = 0; s < kTopSlices; ++s) {
-    const uint32_t o = tops[tl.expert * kTopSlices + s];
+    const uint32_t o = key_tops[s < slices ? s : 0];
     top = o > top ? o : top;
   }
   const int ec = scale_exponent(top);
@@ -1326,7 +1347,7 @@ ColumnsWork columns_work(const ColumnsPlan& p, int n, int64_t m, int groups, int
   w.x = 0;
   w.exps = w.x + align256(t * column_units(m) * 32);  // units in two parts
   w.tops = w.exps + align256(t * 4);
-  w.z = w.tops + align256(static_cast<int64_t>(experts) * kTopSlices * 4);
+  w.z = w.tops + align256(static_cast<int64_t>(experts) * groups * 2 * top_slices(m) * 4);
   w.rz = w.z + align256(2 * t * k * 4);
   w.parts = w.rz + align256(t * k * 4);
   w.end = w.parts + p.part_rows * 2 * k * 4;
@@ -1369,7 +1390,8 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
   float* rz = reinterpret_cast<float*>(a.work + at.rz);
   float* parts = reinterpret_cast<float*>(a.work + at.parts);
   _Float16* units = reinterpret_cast<_Float16*>(a.work + at.x);
-  const int64_t per_expert = a.m * a.groups * 8, slices = static_cast<int64_t>(a.experts) * kTopSlices;
+  const int keys = a.groups * 2;
+  const int64_t slices = static_cast<int64_t>(a.experts) * top_slices(a.m) * ((keys + kSplitT - 1) / kSplitT);
   hipError_t e = hipSuccess;
   if (p.tile) {
     auto split = [&](auto zero) {
@@ -1378,7 +1400,7 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
         constexpr int ROWS = decltype(rows)::value;
         hipLaunchKernelGGL((split_columns_kernel<ROWS, T>), dim3(static_cast<unsigned>((a.t + ROWS - 1) / ROWS + slices)),
                            dim3(kSplitT), 0, s, static_cast<const T*>(a.x), a.ldx, a.x_scales, a.x_group, a.m, a.t, lo ? 2 : 1,
-                           a.centers, per_expert, units, exps, tops);
+                           a.centers, keys, units, exps, tops);
       };
       if (a.t < kManyRows) launch(std::integral_constant<int, 2>());
       else launch(std::integral_constant<int, 8>());

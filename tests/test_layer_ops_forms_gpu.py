@@ -1,6 +1,6 @@
 """The layer operators' further forms on the GPU against float64: every vector length, every tile of the products whole and by
-expert, rows that no expert has, values that are not finite.  Tolerances as in test_layer_ops_gpu, whose helpers these
-tests use; where one differs its derivation stands beside it."""
+expert, rows that no expert has, values that are not finite, matrices of uneven magnitude.  Tolerances as in
+test_layer_ops_gpu, whose helpers these tests use; where one differs its derivation stands beside it."""
 import math
 
 import numpy as np
@@ -146,3 +146,32 @@ def test_experts_of_rotated_weights_beside_rows_of_nobody(n, groups, rot, back):
         case = Case(n, 90, groups, experts=4, rot=rot)
         for dtype, out in (("f16", "f32"), ("e4m3", "bf16")):
             _grouped(case, _ragged(4, each, n), 1, 3, dtype, out, back)
+
+
+# ----------------------------------------------------------------------------- magnitudes
+@pytest.mark.parametrize("t", [1, 9, 15, 16, 40, 70, 130])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_transposed_groups_of_uneven_magnitude(t, out):
+    """The columns of a group come from its own centres: those scaled by a power of two scale the columns, bit for bit,
+    whatever the other groups hold; the same for a factor (where the other one is zero)."""
+    case = Case(256, 300, 3)
+    cu, cv, ce = case.dev
+    x = base._rows(np.random.default_rng(t), t, case.m, "f32")
+
+    def product(centers):
+        y = torch.empty((t, case.k), dtype=base.DT[out], device="cuda")
+        K.kashin_matmul_t(case.plan, cu, cv, centers, x, y, case.work(t, True))
+        return y.to(torch.float32).view(t, 3, 256)
+
+    y = product(ce)
+    by = torch.tensor([2.0 ** -30, 1.0, 2.0 ** -45], device="cuda")
+    assert torch.equal(product((ce.view(300, 3, 8) * by[:, None]).view(-1, 2, 4)), y * by[:, None])
+    for f in (0, 1):
+        one = ce.clone().view(300, 3, 2, 4)
+        one[:, :, 1 - f] = 0.0
+        one[:, 0, 1 - f] = 2.0 ** -6
+        y = product(one.view(-1, 2, 4))
+        other = one.clone()
+        other[:, 0, 1 - f] = 1.0  # group 0's other factor far above
+        other[:, 1:] *= 2.0 ** -40
+        assert torch.equal(product(other.view(-1, 2, 4))[:, 1:], y[:, 1:] * 2.0 ** -40)
