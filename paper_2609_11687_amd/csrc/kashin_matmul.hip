@@ -1099,7 +1099,9 @@ __global__ __launch_bounds__(512, LO ? 2 : 4) void columns_tile_kernel(ProductAr
     ce[at] = *reinterpret_cast<const float4_t*>(a.centers + row * 8 + 4 * f);
   };
   auto decode = [&](int buf, uint32_t codes_of, float4_t centers_of) {
-    const Table tb = make_table(centers_of, cscale);
+    // 0, or NaN where one of the four is not finite: then all are, whichever the codes take
+    const float lost = fmaf(centers_of[0], 0.f, centers_of[1] * 0.f) + fmaf(centers_of[2], 0.f, centers_of[3] * 0.f);
+    const Table tb = make_table(centers_of, cscale + lost);
     const uint32_t word = codes_of >> shift;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {

@@ -175,3 +175,26 @@ def test_transposed_groups_of_uneven_magnitude(t, out):
         other[:, 0, 1 - f] = 1.0  # group 0's other factor far above
         other[:, 1:] *= 2.0 ** -40
         assert torch.equal(product(other.view(-1, 2, 4))[:, 1:], y[:, 1:] * 2.0 ** -40)
+
+
+@pytest.mark.parametrize("t", [3, 12, 20, 70, 130])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("factor", [0, 1])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+def test_products_with_one_centre_that_is_not_finite(t, out, factor, value):
+    """One centre of a row of W_hat: its column is NaN, transposed the columns of its group, whichever entries take that
+    centre, and nothing else."""
+    case = Case(256, 40, 2)
+    cu, cv, ce = case.dev
+    ce = ce.clone()
+    ce[7 * 2 + 1, factor, 2] = value
+    x = base._rows(np.random.default_rng(0), t, case.k, "f32")
+    y = torch.empty((t, 40), dtype=base.DT[out], device="cuda")
+    K.kashin_matmul(case.plan, cu, cv, ce, x, y, case.work(t, False))
+    assert y[:, 7].isnan().all()
+    assert y[:, [i for i in range(40) if i != 7]].isfinite().all()
+    x = base._rows(np.random.default_rng(0), t, 40, "f32")
+    x[0] = 0.0
+    y = torch.empty((t, 512), dtype=base.DT[out], device="cuda")
+    K.kashin_matmul_t(case.plan, cu, cv, ce, x, y, case.work(t, True))
+    assert y[:, 256:].isnan().all() and y[:, :256].isfinite().all()
