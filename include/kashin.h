@@ -352,8 +352,8 @@ int64_t kashin_matmul_workspace_bytes(int32_t n, int64_t m, int32_t groups, int6
  *   work      at least kashin_matmul_workspace_bytes(n, m, groups, t, experts, 0) bytes, 16-byte aligned
  *             (device; its contents on entry do not matter; calls that overlap in time need one each)
  * P x and sums are fp32; the products' operands are exact to about 2^-21 of a row's largest terms.  Where y is
- * bf16 they are rounded to fp16: 2^-11 of each term (up to 33 * 2^-11 of |x| max|centre| a term, typically 3,
- * transposed with fewer than 8 rows a matrix).  A row of x holding NaN or Inf gives a row of NaN, a row of W_hat
+ * bf16 they are rounded to fp16, each by up to 2^-11: 2^-10 of each term (transposed with 8 rows a matrix or more, by
+ * expert with 6; exact as above with fewer).  A row of x holding NaN or Inf gives a row of NaN, a row of W_hat
  * with a centre that is not finite gives a column of NaN (transposed: the columns of its group). */
 int kashin_matmul(const kashin_weights* w, const void* x, int32_t x_dtype, int64_t t, int64_t ldx, const float* x_scales,
                   int32_t x_group, void* y, int32_t y_dtype, int64_t ldy, void* work, int64_t work_bytes, void* stream);

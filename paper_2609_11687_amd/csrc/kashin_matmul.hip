@@ -690,7 +690,9 @@ __global__ __launch_bounds__(512, LO || !ALIGNED ? 2 : 4) void rows_tile_kernel(
 // take a shift and three ands.
 //
 // A workgroup scales by what it meets: max |x| of a row of x into [2^6, 2^7), the largest finite centre into [2^4, 2^5), so
-// that a coefficient times x stays below 2^14.  Products of a bf16 result take the coefficients' hi parts only.
+// that a coefficient times x stays below 1.5 * 2^14.  Both parts of it are taken whatever y's type: for up to 8 rows they cost
+// nothing (hi and lo parts are columns of one operand), and 33 max|centre| |x| rounded to fp16 once would leave a bf16
+// result little better than its own rounding.
 // One row of x, 4096 x 4096: 8.4 MB of codes and 0.3 of centres in 11.3 us, and 3.5 us to join the splits; bound by the loads'
 // latency over the 32 steps of a workgroup, of which three are under way.
 // The tiled kernel's partial maxima of the centres: of each expert's groups and factors (a key: group * 2 + factor), over this
@@ -722,10 +724,10 @@ struct ColumnsPlan {
   int64_t rows, tiles, part_rows;
 };
 
-template <int J, bool LO, class T>
+template <int J, class T>
 __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsPlan pl, XIn<T> x, float* out) {
   constexpr int STEPS = 16;  // columns of a lane's dword
-  constexpr int TT = tile_rows<J>(), JJ = J == 0 ? 1 : J, PARTS = LO && J != 0 ? 2 : 1, CP = 16 * JJ;
+  constexpr int TT = tile_rows<J>(), JJ = J == 0 ? 1 : J, PARTS = J != 0 ? 2 : 1, CP = 16 * JJ;
   __shared__ __align__(16) _Float16 xs[2][4][PARTS][4][CP][8];  // [buffer][function][part][quarter][column of B][row]
   __shared__ uint32_t tops[TT + 1];  // of the rows of x, of the centres
   const Tile tl = find_tile<TT>(a.offsets, a.experts, a.t, blockIdx.y);
@@ -844,7 +846,7 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
     for (int k = 0; k < 4; ++k) {
       *reinterpret_cast<uint32_t*>(&xs[buf][k][0][pair / 4][c][2 * (pair % 4)]) = pair_bits(h[0][k], h[1][k]);
       if constexpr (J == 0) *reinterpret_cast<uint32_t*>(&xs[buf][k][0][pair / 4][c + 8][2 * (pair % 4)]) = pair_bits(l[0][k], l[1][k]);
-      else if constexpr (LO) *reinterpret_cast<uint32_t*>(&xs[buf][k][PARTS - 1][pair / 4][c][2 * (pair % 4)]) = pair_bits(l[0][k], l[1][k]);
+      else *reinterpret_cast<uint32_t*>(&xs[buf][k][1][pair / 4][c][2 * (pair % 4)]) = pair_bits(l[0][k], l[1][k]);
     }
   };
   auto build = [&](const Item& first, int64_t k0, int buf) {
@@ -1317,13 +1319,15 @@ ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, b
   // tiles of at most 16 rows each want their share of `fill`
   const int64_t bound = (fill / one + 1) * 16 + t;
   p.part_rows = most * t < bound ? most * t : bound;
-  // Tiles from 16 rows of x a matrix on, with hi parts alone from 8 (4096 x 4096, us with and without: fp32 results 16 rows of
-  // x 45 and 59, 12 rows 44 and 39, 47 rows 50 and 83; bf16 8 rows 33 and 41, 4 rows 32 and 31; 8 experts, 2048 x 4096: fp32
-  // 16 rows each 88 and 83, 32 rows 90 and 124, bf16 8 rows 53 and 48, 10 rows 53 and 65).  Of 64 rows where 128
+  // Tiles from 16 rows of x a matrix on, with hi parts alone from 8, by expert from 6, whose tiles of eight rows are partly
+  // empty (us with and without: 4096 x 4096, fp32 results, 16 rows of x 45 and 59, 12 rows 44 and 39, 47 rows 50 and 83; bf16
+  // results, 7 rows 33.0 and 34.5, 4 rows 31.9 and 30.2; 1024 x 1024 bf16 7 rows 22.3 and 20.2; 8 experts, 2048 x 4096: fp32
+  // 16 rows each 88 and 83, 32 rows 90 and 124, bf16 7 rows 52 and 61, 5 rows 51 and 58; 64 experts, 1000 x 2048: bf16 7
+  // rows 83 and 98, 5 rows 81 and 74).  Of 64 rows where 128
   // would be half empty; where experts' rows end in a tile's middle 64 also pay up to 128 rows a matrix with hi and lo parts,
   // whose products hide the codes' decoding (8 experts, 2048 x 4096, fp32 results, us with 64 and 128: 400 rows 131 and
   // 152, 700 rows 156 and 191, 1500 rows 288 and 248; bf16: 400 rows 81 and 84, 700 rows 96 and 92).
-  p.tile = each < (lo ? 16 : 8) ? 0 : (grouped ? each < (lo ? 128 : 64) : t <= 64) ? 64 : 128;
+  p.tile = each < (lo ? 16 : grouped ? 6 : 8) ? 0 : (grouped ? each < (lo ? 128 : 64) : t <= 64) ? 64 : 128;
   if (p.tile) {
     p.per_group = (n + kColsN - 1) / kColsN;
     p.tiles = most_tiles(grouped, t, experts, p.tile);
@@ -1333,9 +1337,6 @@ ColumnsPlan plan_columns(int n, int64_t m, int groups, int64_t t, int experts, b
     const int64_t wanted = (512 + others - 1) / others, top = (m + 255) / 256, cut = wanted < top ? wanted : top;
     p.rows = ((m + cut - 1) / cut + 31) / 32 * 32;
     p.splits = static_cast<int>((m + p.rows - 1) / p.rows);
-  } else if (!lo && p.j == 0) {
-    p.j = 1;
-    p.tiles = most_tiles(grouped, t, experts, 16);
   }
   return p;
 }
@@ -1356,7 +1357,7 @@ ColumnsWork columns_work(const ColumnsPlan& p, int n, int64_t m, int groups, int
   return w;
 }
 
-template <int J, bool LO>
+template <int J>
 hipError_t launch_columns(const ProductArgs& a, const ColumnsPlan& p, float* parts, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(p.per_group) * a.groups * 2 * p.splits),
                   static_cast<unsigned>(p.tiles));
@@ -1364,7 +1365,7 @@ hipError_t launch_columns(const ProductArgs& a, const ColumnsPlan& p, float* par
     using T = decltype(zero);
     const XIn<T> x = {static_cast<const T*>(a.x), a.ldx, a.x_scales, a.x_group,
                       a.x_group ? static_cast<int>((a.m + a.x_group - 1) / a.x_group) : 1};
-    hipLaunchKernelGGL((columns_kernel<J, LO, T>), grid, dim3(64 * p.waves), 0, s, a, p, x, parts);
+    hipLaunchKernelGGL((columns_kernel<J, T>), grid, dim3(64 * p.waves), 0, s, a, p, x, parts);
   };
   if (a.x_dtype == KASHIN_E4M3) launch(e4m3_t());
   else with_float_type(a.x_dtype, launch);
@@ -1414,10 +1415,8 @@ hipError_t product_back(const ProductArgs& a, hipStream_t s) {
                            : launch_columns_tile<64, false>(a, p, units, exps, tops, parts, s))
                      : (lo ? launch_columns_tile<128, true>(a, p, units, exps, tops, parts, s)
                            : launch_columns_tile<128, false>(a, p, units, exps, tops, parts, s));
-  } else if (lo) {
-    e = p.j == 0 ? launch_columns<0, true>(a, p, parts, s) : launch_columns<1, true>(a, p, parts, s);
   } else {
-    e = launch_columns<1, false>(a, p, parts, s);
+    e = p.j == 0 ? launch_columns<0>(a, p, parts, s) : launch_columns<1>(a, p, parts, s);
   }
   if (e != hipSuccess) return e;
   const unsigned rows = static_cast<unsigned>(a.t), strips = static_cast<unsigned>((k + 255) / 256);

@@ -198,3 +198,18 @@ def test_products_with_one_centre_that_is_not_finite(t, out, factor, value):
     y = torch.empty((t, 512), dtype=base.DT[out], device="cuda")
     K.kashin_matmul_t(case.plan, cu, cv, ce, x, y, case.work(t, True))
     assert y[:, 256:].isnan().all() and y[:, :256].isfinite().all()
+
+
+@pytest.mark.parametrize("t", [1, 3, 7])
+@pytest.mark.parametrize("n,groups,m", [(512, 1, 200), (256, 3, 1000), (4096, 1, 700)])
+def test_transposed_bf16_results_of_few_rows(n, groups, m, t):
+    """Few rows cost no more with operands of two parts, so nearly every bf16 result is the exact one's rounding.  An fp32
+    result is off by 1e-6 of a typical one at most (NORM).  An entry then rounds elsewhere where a border between two
+    bf16 numbers (2^-8 to 2^-7 of |y| apart) lies within that: 2 * 1e-6 * 2^8 = 5e-4 for a typical entry, about five times
+    that on average over normally distributed ones (smaller entries have closer borders).  1 in 100 is allowed."""
+    case = Case(n, m, groups)
+    for dtype in ("bf16", "f32", "e4m3"):
+        x, got = base._product(case, t, dtype, "bf16", True, 64 if dtype == "e4m3" else 0)
+        base._check(case, got, x, "bf16", True)
+        want = torch.from_numpy(x @ case.w[0]).to(torch.bfloat16)
+        assert (got.cpu() != want).float().mean() <= 0.01, (dtype, (got.cpu() != want).float().mean())
