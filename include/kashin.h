@@ -312,6 +312,7 @@ int kashin_optq_quantize_noalloc(kashin_plan_t plan, float* w_t, int64_t d_in, i
  *   h       t rows of x's type, ldh >= n (device, nullable); h may be x or r (the same rows), any other
  *           overlap with them is KASHIN_E_INVALID
  *   y       t rows of y_dtype KASHIN_F32, _F16, _BF16 or _E4M3, ldy >= n (device); overlaps none of the others
+ *           (column ranges of one buffer, with one leading dimension, do not overlap; h beside x or r as well)
  *   scales  t x ceil(n / group) fp32, or t for group 0 (device): KASHIN_E4M3 only, else null and group 0
  *   group   0, 32, 64, 128 or 256
  * Sums are fp32: a row whose sum of squares passes 3.4e38 gives zeros, and with eps = 0 one whose squares vanish
@@ -348,7 +349,7 @@ int64_t kashin_matmul_workspace_bytes(int32_t n, int64_t m, int32_t groups, int6
  *   x_scales  KASHIN_E4M3: t x ceil(k / x_group) fp32 scales (x_group a multiple of 32), or t (x_group 0: one
  *             for each row); else null and x_group 0 (device)
  *   y         t rows of m, y_dtype KASHIN_F32, _F16 or _BF16, ldy >= m (device); neither y nor work overlaps
- *             another argument
+ *             another argument (column ranges of one buffer, with one leading dimension, do not overlap)
  *   work      at least kashin_matmul_workspace_bytes(n, m, groups, t, experts, 0) bytes, 16-byte aligned
  *             (device; its contents on entry do not matter; calls that overlap in time need one each)
  * P x and sums are fp32; the products' operands are exact to about 2^-21 of a row's largest terms.  Where y is

@@ -712,12 +712,20 @@ namespace {
 
 int64_t elem_size(int32_t dtype) { return dtype == KASHIN_F32 ? 4 : dtype == KASHIN_E4M3 ? 1 : 2; }
 
-// Rows of `width` entries: the addresses from the first entry to behind the last.
+// Rows of `width` entries: the addresses from the first entry to behind the last.  Rows of one leading dimension that lie
+// between each other's (column ranges of one buffer) do not meet although their ranges do.
 struct Span {
   uintptr_t lo, hi;
+  uint64_t pitch, row;  // in bytes; pitch 0: one row
   Span(const void* p, int64_t rows, int64_t ld, int64_t width, int64_t size)
-      : lo(reinterpret_cast<uintptr_t>(p)), hi(p == nullptr || rows == 0 ? lo : lo + ((rows - 1) * ld + width) * size) {}
-  bool meets(const Span& o) const { return lo < o.hi && o.lo < hi; }
+      : lo(reinterpret_cast<uintptr_t>(p)), hi(p == nullptr || rows == 0 ? lo : lo + ((rows - 1) * ld + width) * size),
+        pitch(rows > 1 ? ld * size : 0), row(width * size) {}
+  bool meets(const Span& o) const {
+    if (lo >= o.hi || o.lo >= hi) return false;
+    if (pitch == 0 || pitch != o.pitch) return true;
+    const uint64_t apart = o.lo >= lo ? (o.lo - lo) % pitch : (pitch - (lo - o.lo) % pitch) % pitch;
+    return apart < row || apart + o.row > pitch;  // o's rows begin `apart` behind this one's
+  }
 };
 
 // The plan's device is made current for the call and the caller's restored.
@@ -840,7 +848,7 @@ int kashin_rmsnorm(int64_t t, int32_t n, const void* x, int32_t dtype, int64_t l
   const int64_t esz = elem_size(dtype), per_row = group ? (n + group - 1) / group : 1;
   const Span sx(x, t, ldx, n, esz), sr(r, t, ldr, n, esz), sh(h, t, ldh, n, esz), sy(y, t, ldy, n, elem_size(y_dtype)),
       sw(weight, 1, 0, n, esz), ss(scales, 1, 0, t * per_row, 4);
-  const bool h_is_x = h == x && ldh == ldx, h_is_r = h == r && ldh == ldr;
+  const bool h_is_x = h == x && (ldh == ldx || t == 1), h_is_r = h == r && (ldh == ldr || t == 1);
   if ((sh.meets(sx) && !h_is_x) || (sh.meets(sr) && !h_is_r))
     return fail(KASHIN_E_INVALID, "h overlaps x or r without being the same rows");
   if (sy.meets(sx) || sy.meets(sr) || sy.meets(sh) || sy.meets(sw) || sy.meets(ss) || sh.meets(sw) || sh.meets(ss) ||

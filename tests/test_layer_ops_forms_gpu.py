@@ -1,6 +1,7 @@
 """The layer operators' further forms on the GPU against float64: every vector length, every tile of the products whole and by
-expert, rows that no expert has, values that are not finite, matrices of uneven magnitude.  Tolerances as in
-test_layer_ops_gpu, whose helpers these tests use; where one differs its derivation stands beside it."""
+expert, rows that no expert has, values that are not finite, matrices of uneven magnitude, rows side by side in one
+buffer.  Tolerances as in test_layer_ops_gpu, whose helpers these tests use; where one differs its derivation stands
+beside it."""
 import math
 
 import numpy as np
@@ -213,3 +214,48 @@ def test_transposed_bf16_results_of_few_rows(n, groups, m, t):
         base._check(case, got, x, "bf16", True)
         want = torch.from_numpy(x @ case.w[0]).to(torch.bfloat16)
         assert (got.cpu() != want).float().mean() <= 0.01, (dtype, (got.cpu() != want).float().mean())
+
+
+# ----------------------------------------------------------------------------- rows side by side
+def test_rows_side_by_side_in_one_buffer():
+    """Column ranges of one buffer are rows of the same leading dimension that lie between each other's and do not overlap."""
+    t, n, m = 9, 512, 100
+    rng = np.random.default_rng(0)
+    wide = torch.full((t, 4 * n + 64), 7.0, device="cuda")
+    x, r, h, y = (wide[:, i * n:(i + 1) * n] for i in range(4))
+    s = wide[:, 4 * n:]
+    a, b = (torch.from_numpy(rng.standard_normal((t, n)).astype(np.float32)).cuda() for _ in range(2))
+    x.copy_(a)
+    r.copy_(b)
+    h1, y1 = torch.empty_like(a), torch.empty_like(a)
+    K.kashin_rmsnorm(a, b, None, 1e-5, h1, y1)
+    K.kashin_rmsnorm(x, r, None, 1e-5, h, y)
+    torch.cuda.synchronize()
+    assert torch.equal(h, h1) and torch.equal(y, y1) and torch.equal(x, a) and torch.equal(r, b) and (s == 7).all()
+    case = Case(n, m)
+    for back in (False, True):
+        wx, wy = (m, n) if back else (n, m)
+        f = K.kashin_matmul_t if back else K.kashin_matmul
+        for dtype in ("f32", "f16"):
+            rows = base._rows(rng, t, wx, dtype)
+            z1 = torch.empty((t, wy), dtype=base.DT[dtype], device="cuda")
+            f(case.plan, *case.dev, rows, z1, case.work(t, back))
+            both = torch.full((t, wx + wy + 3), 7.0, dtype=base.DT[dtype], device="cuda")
+            for at_x, at_z in ((0, wx + 3), (wy + 1, 0)):
+                both.fill_(7.0)
+                u, z = both[:, at_x:at_x + wx], both[:, at_z:at_z + wy]
+                u.copy_(rows)
+                f(case.plan, *case.dev, u, z, case.work(t, back))
+                torch.cuda.synchronize()
+                assert torch.equal(z, z1) and torch.equal(u, rows)
+                rest = torch.ones(wx + wy + 3, dtype=torch.bool, device="cuda")
+                rest[at_x:at_x + wx] = False
+                rest[at_z:at_z + wy] = False
+                assert (both[:, rest] == 7).all()
+    # rows that do meet, in one buffer with one leading dimension
+    flat = torch.empty(t * 2 * n + n, device="cuda")
+    x = flat[:t * 2 * n].view(t, 2 * n)[:, :n]
+    for at in (n - 1, 2 * n - m + 1, 2 * n, 0):
+        y = flat[at:at + (t - 1) * 2 * n].view(t - 1, 2 * n)[:, :m]
+        with pytest.raises(K.KashinError, match="overlap"):
+            K.kashin_matmul(case.plan, *case.dev, x[:t - 1], y, case.work(t, False))
