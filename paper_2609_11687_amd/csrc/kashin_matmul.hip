@@ -1469,32 +1469,48 @@ hipError_t launch_product_rows(const ProductArgs& a, const _Float16* frags, cons
   return lo ? launch_rows<4, 2, true>(a, frags, exps, s) : launch_rows<4, 2, false>(a, frags, exps, s);
 }
 
+// Whether P's kernel writes the operands itself: one launch and no P x in memory (4096 x 4096, bf16, 16 rows of x 22.9 -> 19.5
+// us against a pass of its own over x and P x, 2048 rows 198 -> 178; 64 experts 1000 x 2048, 4000 rows 119 -> 102).  Where a
+// row has several groups each pair of them looks for the row's largest entry: up to 2^28 entries looked at in all (4096
+// matrix rows; 16 groups of 256: one row of x 18.0 -> 13.8 us, 1000 rows 125 -> 122; 64 groups of 256: 100 rows, 2^27, 84 -> 76,
+// 1000 rows, 2^30, 453 -> 478).
+bool direct_operands(int n, int groups, int64_t t) { return groups == 1 || t * groups * groups * n <= int64_t(1) << 28; }
+
+struct RowsWork {
+  int64_t wide, px, exps, frags, end;  // px: only where P x passes through memory
+};
+RowsWork rows_work(int n, int groups, int64_t t) {
+  const int64_t rows = align256(t * groups * n * 4);
+  RowsWork w;
+  w.wide = 0;
+  w.px = w.wide + rows;
+  w.exps = w.px + (direct_operands(n, groups, t) ? 0 : rows);
+  w.frags = w.exps + align256(t * 4);
+  w.end = w.frags + 4 * padded_chunks(n, groups) * kUnits * t * 16;
+  return w;
+}
+
 }  // namespace
 
 int64_t product_workspace_bytes(int n, int64_t m, int groups, int64_t t, int experts, bool back) {
-  const int64_t k = static_cast<int64_t>(groups) * n;
   if (t == 0) return 0;
   if (back) return columns_work(plan_columns(n, m, groups, t, experts, experts > 1, true), n, m, groups, t, experts).end;
-  return 2 * align256(t * k * 4) + align256(t * 4) + 4 * padded_chunks(n, groups) * kUnits * t * 16;
+  return rows_work(n, groups, t).end;
 }
 
 hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
   if (a.back) return product_back(a, s);
   const int64_t k = static_cast<int64_t>(a.groups) * a.n;
-  float* wide = reinterpret_cast<float*>(a.work);
-  float* px = reinterpret_cast<float*>(a.work + align256(a.t * k * 4));
-  int32_t* exps = reinterpret_cast<int32_t*>(a.work + 2 * align256(a.t * k * 4));
-  _Float16* frags = reinterpret_cast<_Float16*>(a.work + 2 * align256(a.t * k * 4) + align256(a.t * 4));
-  // bf16 results are rounded by 2^-9 each; operands rounded to fp16 (2^-12) add nothing to speak of
+  const RowsWork at = rows_work(a.n, a.groups, a.t);
+  float* wide = reinterpret_cast<float*>(a.work + at.wide);
+  float* px = reinterpret_cast<float*>(a.work + at.px);
+  int32_t* exps = reinterpret_cast<int32_t*>(a.work + at.exps);
+  _Float16* frags = reinterpret_cast<_Float16*>(a.work + at.frags);
+  // bf16 results are rounded by up to 2^-8 each; operands rounded to fp16 (2^-11 each) add little to that
   const int64_t each = rows_each(a.t, a.experts);
   const bool lo = a.y_dtype != KASHIN_BF16;
   const int parts = lo ? 2 : 1;
-  // P writes the operands itself: one launch and no P x in memory (4096 x 4096, bf16, 16 rows of x 22.9 -> 19.5 us against a
-  // pass of its own over x and P x, 2048 rows 198 -> 178; 64 experts 1000 x 2048, 4000 rows 119 -> 102).  Where a row has
-  // several groups each pair of them looks for the row's largest entry: up to 2^28 entries looked at in all (4096 matrix rows;
-  // 16 groups of 256: one row of x 18.0 -> 13.8 us, 1000 rows 125 -> 122; 64 groups of 256: 100 rows, 2^27, 84 -> 76, 1000
-  // rows, 2^30, 453 -> 478).
-  const bool direct = a.groups == 1 || a.t * a.groups * k <= int64_t(1) << 28;
+  const bool direct = direct_operands(a.n, a.groups, a.t);
   // the caller's rows where the next kernel can read them, else fp32 ones
   XRows x = {a.x, a.ldx, a.x_dtype};
   hipError_t e = hipSuccess;

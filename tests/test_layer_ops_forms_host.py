@@ -1,5 +1,5 @@
-"""Rows of one leading dimension in one buffer: those that meet are refused before any device is touched (those that lie
-between each other's are accepted: test_layer_ops_forms_gpu)."""
+"""Host-side checks of the layer operators.  Rows of one leading dimension in one buffer: those that meet are refused before
+any device is touched (those that lie between each other's are accepted: test_layer_ops_forms_gpu).  Workspaces."""
 import pytest
 
 from paper_2609_11687_amd import kashin as K
@@ -23,3 +23,18 @@ def _norm(t=4, n=512, x=X, r=None, h=None, ldh=LD, y=S, ldy=LD):
 def test_rows_that_meet_are_refused(kw):
     assert _norm(**kw) == K.KASHIN_E_INVALID
     assert "overlap" in K.lib().kashin_last_error().decode()
+
+
+def test_workspace_holds_p_of_x_only_where_it_passes_through_memory():
+    """Two parts of two factors, a row's exponent and one fp32 copy of x, and P x besides for rows of very many groups; never
+    less for more rows."""
+    size = K.kashin_matmul_workspace_bytes
+    up = lambda v: -(-v // 256) * 256  # noqa: E731
+    for n, groups, rows in ((4096, 1, (1, 100, 65536)), (256, 16, (1, 4096)), (64, 128, (1, 256, 257, 60000))):
+        k = n * groups
+        chunks = -(-groups * -(-n // 64) // 4) * 4
+        for t in rows:
+            copies = 1 if groups == 1 or t * groups * k <= 2 ** 28 else 2
+            assert size(n, 1000, groups, t) == copies * up(4 * t * k) + up(4 * t) + 4 * chunks * 8 * t * 16
+    sizes = [size(64, 1000, 128, t) for t in range(600)]
+    assert sizes == sorted(sizes)
