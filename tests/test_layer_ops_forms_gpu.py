@@ -55,6 +55,22 @@ def test_rmsnorm_groups_with_an_infinite_y(n, group):
                 assert lost[:4].all()
 
 
+@pytest.mark.parametrize("n,t", [(8, (1 << 22) + 7), (520, (1 << 20) + 5), (2050, (1 << 20) + 1)])
+def test_rmsnorm_of_more_rows_than_a_grid_holds(n, t):
+    """Workgroups that walk several rows: as calls on parts of the rows, bit for bit."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.empty((t, n), dtype=torch.bfloat16, device="cuda")
+    for part in x.split(1 << 18):
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda"))
+    q, s = torch.empty((t, n), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty((t, 1), device="cuda")
+    K.kashin_rmsnorm(x, None, None, 1e-6, None, q, s)
+    for i in range(0, t, 1 << 18):
+        part = x[i:i + (1 << 18)]
+        q1, s1 = torch.empty_like(q[i:i + (1 << 18)]), torch.empty_like(s[i:i + (1 << 18)])
+        K.kashin_rmsnorm(part, None, None, 1e-6, None, q1, s1)
+        assert torch.equal(q1.view(torch.uint8), q[i:i + (1 << 18)].view(torch.uint8)) and torch.equal(s1, s[i:i + (1 << 18)])
+
+
 # ----------------------------------------------------------------------------- lengths
 @pytest.mark.parametrize("back", [False, True])
 def test_products_of_every_compiled_length(back):
