@@ -315,10 +315,10 @@ int kashin_optq_quantize_noalloc(kashin_plan_t plan, float* w_t, int64_t d_in, i
  *           (column ranges of one buffer, with one leading dimension, do not overlap; h beside x or r as well)
  *   scales  t x ceil(n / group) fp32, or t for group 0 (device): KASHIN_E4M3 only, else null and group 0
  *   group   0, 32, 64, 128 or 256
- * Sums are fp32: a row whose sum of squares passes 3.4e38 gives zeros, and with eps = 0 one whose squares vanish
- * (entries below about 1e-23) infinities, or NaN for its zeros.  A row holding NaN gives NaN, one holding Inf gives NaN there
- * and zeros elsewhere.  In 8 bits, a group with a NaN or an infinite y (weight's too) has scale NaN and zeros.  A
- * group of zeros has scale 0.
+ * Sums are fp32: a row whose sum of squares passes 3.4e38 gives zeros; with eps = 0 a row of entries below about 1e-19
+ * loses bits, and one whose squares vanish (1e-23) gives infinities, or NaN for its zeros.  A row holding NaN gives NaN,
+ * one holding Inf gives NaN there and zeros elsewhere.  In 8 bits, a group with a NaN or an infinite y (by an infinite weight,
+ * say) has scale NaN and zeros.  A group of zeros has scale 0.
  * Plan-free: runs on the current device. */
 int kashin_rmsnorm(int64_t t, int32_t n, const void* x, int32_t dtype, int64_t ldx, const void* r, int64_t ldr,
                    const void* weight, float eps, void* h, int64_t ldh, void* y, int32_t y_dtype, int64_t ldy,
@@ -352,10 +352,13 @@ int64_t kashin_matmul_workspace_bytes(int32_t n, int64_t m, int32_t groups, int6
  *             another argument (column ranges of one buffer, with one leading dimension, do not overlap)
  *   work      at least kashin_matmul_workspace_bytes(n, m, groups, t, experts, 0) bytes, 16-byte aligned
  *             (device; its contents on entry do not matter; calls that overlap in time need one each)
- * P x and sums are fp32; the products' operands are exact to about 2^-21 of a row's largest terms.  Where y is
- * bf16 they are rounded to fp16, each by up to 2^-11: 2^-10 of each term (transposed with 8 rows a matrix or more, by
- * expert with 6; exact as above with fewer).  A row of x holding NaN or Inf gives a row of NaN, a row of W_hat
- * with a centre that is not finite gives a column of NaN (transposed: the columns of its group). */
+ * P x and sums are fp32.  Operands are two fp16 parts: off by up to 2^-22 of their value, or 2^-32 of the row's
+ * largest entry of x and 2^-38 of the largest centre (of the matrix row, transposed of the group and factor), whichever is
+ * more; transposed with few rows (up to 15 a matrix) a row's four centres are combined, 33 * 2^-22 of |x| max|centre| in
+ * all.  Where y is bf16 the operands are fp16 numbers, each off by up to 2^-11: 2^-10 of each term (transposed with 8 rows a
+ * matrix or more, by expert with 6 on average; two parts with fewer).
+ * A row of x holding NaN or Inf gives a row of NaN, a row of W_hat with a centre that is not finite gives a column of NaN
+ * (transposed: the columns of its group). */
 int kashin_matmul(const kashin_weights* w, const void* x, int32_t x_dtype, int64_t t, int64_t ldx, const float* x_scales,
                   int32_t x_group, void* y, int32_t y_dtype, int64_t ldy, void* work, int64_t work_bytes, void* stream);
 

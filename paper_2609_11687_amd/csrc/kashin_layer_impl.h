@@ -9,8 +9,9 @@
 // a small part; the operands of one row leave as 32-byte pieces of 32 KB.  Hence x's own operands are written by workgroups
 // of their own, beside those that transform; the rows are asked for before the operator's constants (the plain P
 // kernel loads its constants first, once for the many pairs that a workgroup walks); a row without a neighbour is loaded
-// and written alone.  2048 bf16 rows of 4096 (50 MB in and out) take 39 us, against 31 + 29 us of P x into memory
-// and a pass over x and P x.
+// and written alone.  2048 bf16 rows of 4096 (50 MB in and out) take 33 us among other calls (39 after a pause, against
+// 31 + 29 us of P x into memory and a pass over x and P x), of which the bytes would take 10: the vector ALU issues in
+// 59 % of the cycles and LDS works in 44 %.
 #pragma once
 
 #include "kashin_rows.h"
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(C::T) __attribute__((amdgpu_waves_per_eu(C::W))) vo
   }
 }
 
-// y = zu + P zv: the end of the transposed products (one row of 4096: 11 us, 509 rows 16; reading zu and zv and writing y would
+// y = zu + P zv: the end of the transposed products (one row of 4096: 11 us, 509 rows 15; reading zu and zv and writing y would
 // take 4 us there, the transform's latency of a pair a compute unit the rest).  A workgroup walks pairs of vectors; a vector passes through LDS into
 // row order, where zu is added and y written in 16-byte pieces.
 template <class C>

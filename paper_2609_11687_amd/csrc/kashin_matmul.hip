@@ -284,9 +284,10 @@ __global__ __launch_bounds__(kSplitT) void split_rows_kernel(XRows x, const floa
 // rows, whose hi parts are B's columns 0 .. 7 and lo parts columns 8 .. 15, so that two instructions give all four products
 // (against three for 16 rows).  LO: both operands in two parts; without it (J > 0) in one.  ALIGNED: n is a multiple of 256, so
 // that a slab lies in one group and no chunk is short: addresses and branches are scalar then.
-// One row of x, 11008 x 4096: 22.5 MB of codes in 12.5 us (1.8 TB/s; 4.4 us at the rate of a copy).  Bound by the decoding
-// (four byte selections for eight values, every instruction in a wave's own time) and by what a launch of eight waves a
-// workgroup waits for first: the centres' scale and the joining of the waves' sums.
+// One row of x, 11008 x 4096: 22.5 MB of codes in 12.0 us (1.9 TB/s; 4.4 us at the rate of a copy).  No unit is full: the
+// vector ALU issues in 44 % of the cycles (mostly the decoding: four byte selections for eight values), the matrix units work in
+// 11 %; the rest is waiting for codes and for what a launch of eight waves a workgroup needs first and last, the
+// centres' scale and the joining of the waves' sums.
 template <int J>
 constexpr int tile_rows() { return J == 0 ? 8 : 16 * J; }
 
@@ -512,9 +513,11 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
 
-// Two workgroups a unit where hi parts alone leave room for it (65 KB of LDS, 128 registers).  Bound by the matrix
-// instructions: 2048 rows of x, 11008 x 4096, bf16 result, 369 GFLOP of [x | P x] [U | V]^T in 393 us, 940 TFLOP/s
-// (one workgroup a unit and addresses of 64 bits for x 455).
+// Two workgroups a unit where hi parts alone leave room for it (65 KB of LDS, 128 registers).  2048 rows of x, 11008 x 4096, bf16
+// result: 369 GFLOP of [x | P x] [U | V]^T in 359 us among other calls, 1.03 PFLOP/s, 95 % of what a large fp16 product
+// reaches here (after a pause 393 us, and 455 with one workgroup a unit and addresses of 64 bits for x); the matrix units work in
+// 67 % of the cycles, the vector ALU issues in 55 %.  fp16 result, three products each: 865 us, 1.28 PFLOP/s.  K in groups of 10000 (no
+// multiple of 256: all loads are waited for each step, one workgroup a unit), 4096 matrix rows, bf16: 394 us, 0.85 PFLOP/s.
 template <int TT, bool LO, bool ALIGNED>
 __global__ __launch_bounds__(512, LO || !ALIGNED ? 2 : 4) void rows_tile_kernel(ProductArgs a, const _Float16* frags, const int32_t* exps) {
   constexpr int PARTS = LO ? 2 : 1, SU = 2 * kUnits;  // units of a slab: two chunks
@@ -693,8 +696,8 @@ __global__ __launch_bounds__(512, LO || !ALIGNED ? 2 : 4) void rows_tile_kernel(
 // that a coefficient times x stays below 1.5 * 2^14.  Both parts of it are taken whatever y's type: for up to 8 rows they cost
 // nothing (hi and lo parts are columns of one operand), and 33 max|centre| |x| rounded to fp16 once would leave a bf16
 // result little better than its own rounding.
-// One row of x, 4096 x 4096: 8.4 MB of codes and 0.3 of centres in 11.3 us, and 3.5 us to join the splits; bound by the loads'
-// latency over the 32 steps of a workgroup, of which three are under way.
+// One row of x, 4096 x 4096: 8.4 MB of codes and 0.3 of centres in 10.5 us, and 3.5 us to join the splits; bound by the loads'
+// latency over the steps of a workgroup, of which three are under way (vector ALU 40 % of the cycles, matrix units 14 %).
 // The tiled kernel's partial maxima of the centres: of each expert's groups and factors (a key: group * 2 + factor), over this
 // many slices of its matrix rows.
 constexpr int kTopSlices = 16;
@@ -955,9 +958,10 @@ __global__ __launch_bounds__(512, 2) void columns_kernel(ProductArgs a, ColumnsP
 // eight matrix rows).  A dword's codes lie in LDS in the order they come out of the tables, 0 4 8 12 1 5 9 13 ..: column
 // 16 d + p / 4 + 4 (p % 4) at place p, which the stores undo.
 // x comes as units of eight matrix rows: units[part][unit][row of x][8], scaled as for x W^T.
-// 509 rows of x, 11008 x 4096, bf16 result: 92 GFLOP in 122 us, 750 TFLOP/s (128-row tiles, two workgroups a unit: 142 us
-// with the two registers more that leave room for one); bound by the LDS traffic of the decoded codes beside the matrix
-// instructions.
+// 509 rows of x, 11008 x 4096, bf16 result, among other calls: 92 GFLOP in 115 us, 800 TFLOP/s (128-row tiles, two workgroups
+// a unit; 142 us where 122 were measured with the two registers more that leave room for one).  No unit is full: matrix units 42 %
+// of the cycles, LDS 43 % (a quarter of that on bank conflicts), vector ALU 48 %; what the waves wait for is each other, at the
+// barrier of every step.  fp16 result, three products each: 252 us, 1.09 PFLOP/s.
 constexpr int kColsM = 32, kColsN = 256, kColsLd = kColsN + 32;  // 576-byte rows: four of them on 64 banks
 using short4_t = short __attribute__((ext_vector_type(4)));
 
