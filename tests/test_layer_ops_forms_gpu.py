@@ -275,3 +275,98 @@ def test_rows_side_by_side_in_one_buffer():
         y = flat[at:at + (t - 1) * 2 * n].view(t - 1, 2 * n)[:, :m]
         with pytest.raises(K.KashinError, match="overlap"):
             K.kashin_matmul(case.plan, *case.dev, x[:t - 1], y, case.work(t, False))
+
+
+# ----------------------------------------------------------------------------- the largest sizes
+def test_products_of_the_most_matrix_rows():
+    """2^24 matrix rows, 4.3 GB of codes a factor: as the products of parts of the matrix.  Transposed, a sum of 2^24 terms:
+    a split's chain of up to 1024 steps of 7 additions and at most 512 splits, 2^-24 (sqrt(7168 / 6) + sqrt(512 / 6)) =
+    2.6e-6 of a typical result; the parts' own sums are shorter.  Four times that is allowed."""
+    n, m, t = 1024, 1 << 24, 2
+    plan = K.kashin_plan(n, 3, 1)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    cu, cv = torch.empty((2, m, n // 4), dtype=torch.uint8, device="cuda")
+    for c in (cu, cv):
+        for part in c.split(1 << 20):
+            part.random_(0, 256, generator=g)
+    ce = (torch.randn((m, 2, 4), generator=g, device="cuda") * 0.02).sort(-1).values
+
+    def run(f, x, lo, hi, width):
+        y = torch.empty((t, width), device="cuda")
+        back = f is K.kashin_matmul_t
+        work = torch.empty(K.kashin_matmul_workspace_bytes(n, hi - lo, 1, t, 1, back), dtype=torch.uint8, device="cuda")
+        f(plan, cu[lo:hi], cv[lo:hi], ce[lo:hi], x, y, work)
+        return y
+    x = torch.randn((t, n), generator=g, device="cuda")
+    y = run(K.kashin_matmul, x, 0, m, m)
+    for lo in (0, (1 << 23) - 256, m - 512):
+        assert torch.equal(y[:, lo:lo + 512], run(K.kashin_matmul, x, lo, lo + 512, 512)), lo
+    x = torch.randn((t, m), generator=g, device="cuda")
+    y = run(K.kashin_matmul_t, x, 0, m, n).double()
+    step = 1 << 20
+    want = sum(run(K.kashin_matmul_t, x[:, lo:lo + step], lo, lo + step, n).double() for lo in range(0, m, step))
+    assert (y - want).norm() <= 4 * 2.6e-6 * want.norm()
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_products_of_the_most_rows(back):
+    case = Case(64, 70)
+    t = 1 << 16
+    for dtype, out in (("bf16", "bf16"), ("f16", "f32")):
+        x, y = base._product(case, t, dtype, out, back)
+        for part in (slice(0, 300), slice(t // 2 - 100, t // 2 + 100), slice(t - 300, t)):
+            base._check(case, y[part], x[part], out, back)
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_products_of_the_longest_rows(back):
+    case = Case(16384, 20, 64)
+    for t, dtype, out in ((2, "f32", "f32"), (20, "bf16", "f32")):
+        x, y = base._product(case, t, dtype, out, back)
+        base._check(case, y, x, out, back)
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_the_most_experts(back):
+    case = Case(64, 16, 2, experts=1024)
+    for each in (1, 30):
+        _grouped(case, _ragged(1024, each, each), 2, 1, "bf16", "f32", back)
+
+
+# ----------------------------------------------------------------------------- graphs
+def test_captured_rotated_products_replay():
+    """Rotated products in tiles and by expert with bf16 results in one captured graph: every replay as the eager calls, bit for
+    bit, with eager work on other inputs in between."""
+    case, ex = Case(512, 700, rot=4), Case(256, 130, 2, experts=3, rot=9)
+    t = 200
+    rng = np.random.default_rng(0)
+    off = torch.tensor([1, 90, 90, 190], device="cuda")
+
+    def state():
+        z = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+        return {"x": z(t, 512), "y": z(t, 700), "z": z(t, 512), "e": z(t, 130), "et": z(t, 512),
+                "work": [case.work(t, False), case.work(t, True), ex.work(t, False), ex.work(t, True)]}
+
+    def step(s):
+        K.kashin_matmul(case.plan, *case.dev, s["x"], s["y"], s["work"][0], rot_seed=case.rot)
+        K.kashin_matmul_t(case.plan, *case.dev, s["y"], s["z"], s["work"][1], rot_seed=case.rot)
+        K.kashin_matmul_experts(ex.plan, *ex.dev, off, s["z"], s["e"], s["work"][2], rot_seed=ex.rot)
+        K.kashin_matmul_experts(ex.plan, *ex.dev, off, s["e"], s["et"], s["work"][3], True, rot_seed=ex.rot)
+
+    s, eager = state(), state()
+    step(eager)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(s)
+    for i in range(4):
+        x = base._rows(rng, t, 512, "bf16")
+        s["x"].copy_(x)
+        eager["x"].copy_(x)
+        graph.replay()
+        step(eager)
+        torch.cuda.synchronize()
+        for key in ("y", "z", "e", "et"):
+            assert s[key].isfinite().all() and torch.equal(s[key].view(torch.uint8), eager[key].view(torch.uint8)), (i, key)
